@@ -447,6 +447,129 @@ rmsmp_status rmsmp_gemm_builtin_scratch(const rmsmp_layer* layer, const void* d_
                                         rmsmp_out_layout out_layout, int32_t* d_acc, void* stream);
 
 /*
+ * Linear layers of 4-bit weights with a scale for every few inputs, on floating-point activations.  The row-wise layers
+ * above give a whole row one scale and multiply 4-bit activations; the 4-bit weights that language models are kept in have
+ * a scale, and often a zero point, for every `group` consecutive inputs of a row, and their activations stay as they are:
+ *   y[n][m] = sum_k s[m][k / group] * (u[m][k] - z[m][k / group]) * x[n][k],       u, z in 0..15
+ * RMSMP_GS4_SYM has z = 8 everywhere (the Fixed-4 rows of Eq. 1, group by group); RMSMP_GS4_ZERO stores one per group.
+ * A layer holds E matrices of M rows and K inputs: E = 1 is a plain linear layer, more are the experts of one layer.
+ * Codes times activations are summed in fp32 over 32, 64 or 128 inputs (the largest of these that divides the group), each
+ * such sum is multiplied by its scale, and those are summed in fp32; the result is rounded once, to y's type.  A sum of codes
+ * times activations beyond fp32's range is infinite even where the scale would bring it back.  Nothing else is rounded: codes are exact in
+ * fp16 and bf16, and an fp32 activation is multiplied as three bf16 numbers that add up to it.
+ *
+ * Packed buffer: 256-byte header (device status word at byte 64, see rmsmp_last_device_status), then
+ *   codes   [E][ceil(M/16)][Kp/64][32][16] bytes, Kp = K rounded up to 128: lane 4g + c's 16 bytes of a block of 16 rows and
+ *           64 inputs, as four words.  Word 2b + j holds rows g and g + 8, inputs 32b + 8c + 4j + i (i = 0..3): nibble
+ *           (i / 2) * 2 + (row >= 8) + 4 * (i & 1).  Codes beyond K and M stand for zero.
+ *   scales  [E][ceil(M/16)][Kp/128][8][n][2], n = 1, 2 or 4 sums for every 128 inputs: rows g and g + 8
+ *   zeros   [E][ceil(M/16)][Kp/128][8][n] bytes (RMSMP_GS4_ZERO only): row g's in the low, row g + 8's in the high half
+ */
+typedef enum { RMSMP_F32 = 0, RMSMP_F16 = 1, RMSMP_BF16 = 2 } rmsmp_dtype;
+typedef enum { RMSMP_GS4_SYM = 0, RMSMP_GS4_ZERO = 1 } rmsmp_gs4_mode;
+typedef struct rmsmp_gs4_layer {
+    uint32_t magic;             /* set by rmsmp_gs4_layer_init */
+    int32_t E, M, K;            /* matrices; rows and inputs of each */
+    int32_t group;              /* consecutive inputs of a row that share a scale */
+    int32_t mode, scale_type;   /* rmsmp_gs4_mode; RMSMP_F16 or RMSMP_BF16 */
+    int32_t Kp, tiles;          /* K rounded up to 128; ceil(M/16) */
+    int32_t sums;               /* sums for every 128 inputs: 1, 2 or 4 */
+    uint64_t off_codes, off_scales, off_zeros;
+    uint64_t packed_bytes;      /* size the packed buffer must have */
+} rmsmp_gs4_layer;
+
+/*
+ * Describe E matrices of M rows and K inputs.  Host only.  Limits: 1 <= E <= 4096, 1 <= M, K <= 2^20, group a multiple of 32 in
+ * 32..2^20 (it may exceed K: one scale a row; the last group of a row may be cut short).  Errors: NULL, SHAPE, SCHEME (mode, scale_type).
+ */
+rmsmp_status rmsmp_gs4_layer_init(rmsmp_gs4_layer* layer, int E, int M, int K, int group, rmsmp_gs4_mode mode,
+                                  rmsmp_dtype scale_type);
+
+/*
+ * Quantize and pack weights d_W, [E][M][K] of w_type.  In fp32, per group:
+ *   SYM:   s = max|w| / 7 rounded to scale_type,  u = 8 + clip(round_half_even(w / s), -7, 7)
+ *   ZERO:  lo = min(w, 0), hi = max(w, 0), s = (hi - lo) / 15 rounded, z = clip(round_half_even(-lo / s), 0, 15),
+ *          u = clip(round_half_even(w / s) + z, 0, 15)
+ * The scale is rounded before the codes are chosen, so that what is stored is the nearest to w that it can be.  A scale that overflows
+ * scale_type is its largest finite number; one that rounds to zero stays zero, with u = z (8).  Weights are finite; the codes and
+ * scale of a group that holds an infinity or NaN are unspecified.
+ * Errors: NULL, BAD_LAYER, SCHEME (w_type), BUFFER_TOO_SMALL, ALIGN (d_packed 256 bytes, d_W its type's size), ARCH, CUDA.
+ */
+rmsmp_status rmsmp_gs4_quantize_pack(const rmsmp_gs4_layer* layer, const void* d_W, rmsmp_dtype w_type, void* d_packed,
+                                     size_t packed_bytes, void* stream);
+
+/*
+ * Pack weights that are quantized already: d_codes [E][M][K] bytes (the low four bits count), d_scale [E][M][G] of scale_type,
+ * d_zero [E][M][G] bytes (low four bits; RMSMP_GS4_ZERO only, ignored otherwise), G = ceil(K / group).  Scales may be any number.
+ * rmsmp_gs4_unpack gives the same three back (d_scale and d_zero may be NULL; zeros of a SYM layer are written as 8).
+ * Errors: NULL, BAD_LAYER, BUFFER_TOO_SMALL, ALIGN, ARCH, CUDA.
+ */
+rmsmp_status rmsmp_gs4_pack_codes(const rmsmp_gs4_layer* layer, const uint8_t* d_codes, const void* d_scale,
+                                  const uint8_t* d_zero, void* d_packed, size_t packed_bytes, void* stream);
+rmsmp_status rmsmp_gs4_unpack(const rmsmp_gs4_layer* layer, const void* d_packed, uint8_t* d_codes, void* d_scale,
+                              uint8_t* d_zero, void* stream);
+
+/*
+ * The product, for one token or many.  d_x: [N][ld_x] of x_type, ld_x >= K; d_y: [N][ld_y] of y_type, ld_y >= M; both need only their
+ * type's alignment (16-byte aligned rows are read faster).  The layer has E = 1.  N = 0 does nothing.
+ * Columns of d_x from K and of d_y from M on are not touched.  d_y must not overlap d_x.
+ * Errors: NULL, BAD_LAYER, SCHEME (types), SHAPE (E > 1, N < 0 or > 2^30, leading dimensions), ALIGN, ARCH, CUDA.
+ */
+rmsmp_status rmsmp_gs4_gemm(const rmsmp_gs4_layer* layer, const void* d_packed, const void* d_x, rmsmp_dtype x_type, int64_t N,
+                            int64_t ld_x, void* d_y, rmsmp_dtype y_type, int64_t ld_y, void* stream);
+
+/*
+ * The product of tokens sorted by expert, by matrices that the device alone knows the tokens of: for every expert e and
+ * row p in d_offsets[e] <= p < d_offsets[e + 1]
+ *   y[p] = W_e x[d_rows[p]]                  (d_rows NULL: x[p])
+ * d_offsets: E + 1 device int32 that do not fall; they are cut to 0..R.  d_x has x_rows rows; a d_rows entry outside 0..x_rows-1
+ * stands for a row of zeros.  R: rows of d_y (a capacity: the host need not know how many are used).  Rows that belong to no
+ * expert are left as they were.  Errors: as rmsmp_gs4_gemm (any E).
+ */
+rmsmp_status rmsmp_gs4_gemm_experts(const rmsmp_gs4_layer* layer, const void* d_packed, const void* d_x, rmsmp_dtype x_type,
+                                    int64_t x_rows, int64_t ld_x, const int32_t* d_rows, const int32_t* d_offsets, int64_t R,
+                                    void* d_y, rmsmp_dtype y_type, int64_t ld_y, void* stream);
+
+/*
+ * Tokens sorted by expert.  d_ids: [T][k] int32, the experts that each token chose; an id outside 0..E-1 is a pair that goes
+ * nowhere (a padded token).  Pairs are ordered by (expert, t * k + j), the same for every run:
+ *   d_offsets[e]    E + 1 int32: first position of expert e; d_offsets[E] = pairs that have a place
+ *   d_rows[p]       T * k int32: token of sorted position p, -1 from d_offsets[E] on
+ *   d_place[t][j]   T * k int32: position of the pair, -1 if it has none
+ * A token may name an expert twice.  One launch, no scratch.  T = 0 gives E + 1 zeros.
+ * Limits: 1 <= E <= 1024, 1 <= k <= 1024, T * k <= 2^30.  Errors: NULL, SHAPE, ALIGN, ARCH, CUDA.
+ */
+rmsmp_status rmsmp_expert_sort(const int32_t* d_ids, int64_t T, int k, int E, int32_t* d_offsets, int32_t* d_rows, int32_t* d_place,
+                               void* stream);
+
+/*
+ * Rows of tokens in sorted order: xs[p] = x[d_rows[p]] for p < R; rows whose entry lies outside 0..x_rows-1 are left as they were.
+ * [x_rows][ld_x] and [R][ld_xs] of `type`, H columns.  (rmsmp_gs4_gemm_experts takes d_rows itself and needs no copy; a program
+ * that keeps the rows for a gradient, or multiplies them by something else, does.)  Its gradient is rmsmp_expert_combine
+ * without weights: dx[t] = sum_j dxs[d_place[t][j]].  Errors: NULL, SCHEME (type), SHAPE, ALIGN (the type's size), ARCH, CUDA.
+ */
+rmsmp_status rmsmp_expert_gather(const void* d_x, rmsmp_dtype type, int64_t x_rows, int64_t H, int64_t ld_x, const int32_t* d_rows,
+                                 int64_t R, void* d_xs, int64_t ld_xs, void* stream);
+
+/*
+ * Back to tokens: y[t] = sum_j w[t][j] * ys[d_place[t][j]], summed in fp32 in the order of j, rounded once.  d_w: [T][k] fp32, or NULL for ones.
+ * Places outside 0..R-1 are skipped whatever their weight; a token without any gets zeros.  [R][ld_ys], [T][ld_y] of `type`.
+ * Errors: as rmsmp_expert_gather.  Limits: k <= 1024.
+ */
+rmsmp_status rmsmp_expert_combine(const void* d_ys, rmsmp_dtype type, int64_t R, int64_t H, int64_t ld_ys, const int32_t* d_place,
+                                  const float* d_w, int64_t T, int k, void* d_y, int64_t ld_y, void* stream);
+
+/*
+ * The gradient of rmsmp_expert_combine: dys[d_place[t][j]] = w[t][j] * dy[t] and dw[t][j] = <dy[t], ys[d_place[t][j]]> (fp32 sums, a fixed order).
+ * A pair without a place has dw = 0; rows of dys that no pair has are left as they were.  d_w NULL: ones.  d_dys or d_dw may be NULL if not
+ * wanted (not both; d_ys may be NULL without d_dw).  Two pairs with one place, which rmsmp_expert_sort never gives, leave one of their rows.
+ * Errors: as rmsmp_expert_gather.
+ */
+rmsmp_status rmsmp_expert_combine_backward(const void* d_dy, rmsmp_dtype type, int64_t T, int k, int64_t H, int64_t ld_dy,
+                                           const void* d_ys, int64_t R, int64_t ld_ys, const int32_t* d_place, const float* d_w,
+                                           void* d_dys, int64_t ld_dys, float* d_dw, void* stream);
+
+/*
  * Read the device status word of a packed buffer (synchronises the stream; the paper, which
  * describes an FPGA datapath, has no counterpart).  Kernels never
  * trap: a bounded wait that runs out stores RMSMP_ERR_TIMEOUT there and the kernel returns.

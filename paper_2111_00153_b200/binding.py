@@ -23,6 +23,8 @@ POT_NEAREST, POT_LOG2 = 0, 1
 OUT_NM, OUT_MN = 0, 1
 W_LINEAR, W_CONV_OIHW = 0, 1
 VARIANT_AUTO, VARIANT_TENSOR, VARIANT_SIMT, VARIANT_SHIFTADD, VARIANT_SIMPLE = 0, 1, 2, 3, 4
+F32, F16, BF16 = 0, 1, 2
+GS4_SYM, GS4_ZERO = 0, 1
 (ERR_NULL, ERR_SHAPE, ERR_SCHEME, ERR_SCALE, ERR_ALIGN, ERR_BUFFER_TOO_SMALL, ERR_ARCH, ERR_CUDA,
  ERR_TIMEOUT, ERR_BAD_LAYER, ERR_VARIANT) = range(1, 12)
 
@@ -34,6 +36,8 @@ EXPORTS = (
     "rmsmp_conv_implicit_workspace", "rmsmp_gemm_builtin_scratch", "rmsmp_grouped_table_bytes",
     "rmsmp_gemm_grouped", "rmsmp_gemm_workspace_requant", "rmsmp_conv_implicit_workspace_requant",
     "rmsmp_conv_depthwise", "rmsmp_im2col_codes", "rmsmp_layer_init_ratio", "rmsmp_assign_scratch_bytes", "rmsmp_assign_quantize_pack", "rmsmp_selftest_bounded_wait", "rmsmp_grouped_plan_bytes", "rmsmp_gemm_grouped_prepare", "rmsmp_gemm_grouped_launch",
+    "rmsmp_gs4_layer_init", "rmsmp_gs4_quantize_pack", "rmsmp_gs4_pack_codes", "rmsmp_gs4_unpack", "rmsmp_gs4_gemm", "rmsmp_gs4_gemm_experts",
+    "rmsmp_expert_sort", "rmsmp_expert_gather", "rmsmp_expert_combine", "rmsmp_expert_combine_backward",
 )
 
 
@@ -67,6 +71,15 @@ class rmsmp_grouped_plan(C.Structure):
     _fields_ = [
         ("magic", C.c_uint32), ("count", C.c_int32), ("grid", C.c_int32), ("smem_bytes", C.c_uint32),
         ("device", C.c_int32), ("conv_grid", C.c_int32), ("d_table", C.c_void_p), ("table_bytes", C.c_uint64),
+    ]
+
+
+class rmsmp_gs4_layer(C.Structure):
+    _fields_ = [
+        ("magic", C.c_uint32),
+        ("E", C.c_int32), ("M", C.c_int32), ("K", C.c_int32), ("group", C.c_int32),
+        ("mode", C.c_int32), ("scale_type", C.c_int32), ("Kp", C.c_int32), ("tiles", C.c_int32), ("sums", C.c_int32),
+        ("off_codes", C.c_uint64), ("off_scales", C.c_uint64), ("off_zeros", C.c_uint64), ("packed_bytes", C.c_uint64),
     ]
 
 
@@ -131,6 +144,17 @@ def lib() -> C.CDLL:
         L.rmsmp_assign_scratch_bytes.argtypes = [i32, C.POINTER(C.c_size_t)]
         L.rmsmp_assign_quantize_pack.argtypes = [vp, i32, C.POINTER(rmsmp_layer), i32, i32, i32, vp, i32, vp, C.c_size_t,
                                                  vp, C.c_size_t, vp, vp, vp]
+        L.rmsmp_gs4_layer_init.argtypes = [C.POINTER(rmsmp_gs4_layer), i32, i32, i32, i32, i32, i32]
+        gs4 = C.POINTER(rmsmp_gs4_layer)
+        L.rmsmp_gs4_quantize_pack.argtypes = [gs4, vp, i32, vp, C.c_size_t, vp]
+        L.rmsmp_gs4_pack_codes.argtypes = [gs4, vp, vp, vp, vp, C.c_size_t, vp]
+        L.rmsmp_gs4_unpack.argtypes = [gs4, vp, vp, vp, vp, vp]
+        L.rmsmp_gs4_gemm.argtypes = [gs4, vp, vp, i32, i64, i64, vp, i32, i64, vp]
+        L.rmsmp_gs4_gemm_experts.argtypes = [gs4, vp, vp, i32, i64, i64, vp, vp, i64, vp, i32, i64, vp]
+        L.rmsmp_expert_sort.argtypes = [vp, i64, i32, i32, vp, vp, vp, vp]
+        L.rmsmp_expert_gather.argtypes = [vp, i32, i64, i64, i64, vp, i64, vp, i64, vp]
+        L.rmsmp_expert_combine.argtypes = [vp, i32, i64, i64, i64, vp, vp, i64, i32, vp, i64, vp]
+        L.rmsmp_expert_combine_backward.argtypes = [vp, i32, i64, i32, i64, i64, vp, i64, i64, vp, vp, vp, i64, vp, vp]
         L.rmsmp_selftest_bounded_wait.argtypes = [i64, vp, vp]
         L.rmsmp_measure_mma_peak.argtypes = [i32, i32, i32, vp, C.POINTER(C.c_float), C.POINTER(C.c_float), vp]
         _lib = L
@@ -207,6 +231,15 @@ _NATIVE = (
     "rmsmp_assign_quantize_pack",
     "rmsmp_quantize_pack",
     "rmsmp_gemm_grouped_launch",
+    "rmsmp_gs4_quantize_pack",
+    "rmsmp_gs4_pack_codes",
+    "rmsmp_gs4_unpack",
+    "rmsmp_gs4_gemm",
+    "rmsmp_gs4_gemm_experts",
+    "rmsmp_expert_sort",
+    "rmsmp_expert_gather",
+    "rmsmp_expert_combine",
+    "rmsmp_expert_combine_backward",
 )
 
 
@@ -355,6 +388,13 @@ def rmsmp_assign_scratch_bytes(M: int) -> int:
     n = C.c_size_t(0)
     _check(lib().rmsmp_assign_scratch_bytes(M, C.byref(n)), "rmsmp_assign_scratch_bytes")
     return n.value
+
+
+def rmsmp_gs4_layer_init(E: int, M: int, K: int, group: int, mode: int = GS4_SYM, scale_type: int = BF16) -> rmsmp_gs4_layer:
+    """Describes E matrices of M rows and K inputs in 4 bits, with a scale for every `group` inputs of a row."""
+    layer = rmsmp_gs4_layer()
+    _check(lib().rmsmp_gs4_layer_init(C.byref(layer), E, M, K, group, mode, scale_type), "rmsmp_gs4_layer_init")
+    return layer
 
 
 def rmsmp_selftest_bounded_wait(limit_cycles: int, d_status_word, stream=None):

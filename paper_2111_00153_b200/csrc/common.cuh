@@ -67,6 +67,7 @@ struct Problem {
 // beyond the tables (kMaxDevices).
 constexpr int kMaxDevices = 64;
 int device_ordinal();
+rmsmp_status arch_status();   // whether the current device is one that the kernels run on (cached per ordinal)
 int sm_count();               // SMs of the current device (cached per ordinal)
 // Calls cudaFuncSetAttribute(MaxDynamicSharedMemorySize) for `fn` once per device: `done` is the
 // kernel's own table of kMaxDevices flags.  Returns false if the attribute could not be set.

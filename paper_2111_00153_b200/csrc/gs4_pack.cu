@@ -1,0 +1,203 @@
+// Packing of 4-bit weights with a scale for every group of inputs (layout: rmsmp.h), from fp32/fp16/bf16 weights or from codes and
+// scales that are there already.  Set-up work: one pass for the scales (a warp per row and group: a maximum), one for the codes (a thread
+// per word of eight), bound by reading the weights twice.  Launched the ordinary way and without letting dependents start early, as every
+// writer of packed buffers is.
+#include <algorithm>
+#include "gs4.cuh"
+
+namespace rmsmp {
+
+namespace {
+
+constexpr int kThreads = 256;
+
+struct PackArgs {
+    const void* w;               // weights (quantize) or null
+    const uint8_t* codes_in;     // codes, scales, zeros (pack)
+    const void* scale_in;
+    const uint8_t* zero_in;
+    uint8_t *codes, *scales, *zeros;
+    int M, K, Kp, tiles, E, group, sums, scale_bf16, w_type, G;
+};
+
+__device__ __forceinline__ int64_t scale_index(const PackArgs& a, int64_t et, int g, int chunk)      // of the pair (rows g, g + 8)
+{
+    return ((et * (a.Kp / 128) + chunk / a.sums) * 8 + g) * a.sums + chunk % a.sums;
+}
+
+__device__ __forceinline__ float warp_max(float v)
+{
+    for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+    return v;
+}
+
+// one warp: rows g and g + 8 of a block of 16, one group
+__global__ void __launch_bounds__(kThreads) gs4_scales_kernel(const PackArgs a)
+{
+    const int lane = threadIdx.x & 31;
+    const int64_t items = (int64_t)a.E * a.tiles * 8 * a.G;
+    for (int64_t it = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); it < items; it += (int64_t)gridDim.x * (kThreads / 32)) {
+        const int grp = (int)(it % a.G);
+        const int g = (int)(it / a.G % 8);
+        const int64_t et = it / a.G / 8;
+        const int64_t e = et / a.tiles;
+        const int m0 = (int)(et % a.tiles) * 16 + g;
+        uint32_t s2[2] = {0, 0}, z2[2] = {0, 0};
+        for (int h = 0; h < 2; ++h) {
+            const int m = m0 + 8 * h;
+            if (m >= a.M) continue;
+            const int64_t row = e * a.M + m;
+            if (!a.w) {
+                s2[h] = static_cast<const uint16_t*>(a.scale_in)[row * a.G + grp];
+                if (a.zeros) z2[h] = a.zero_in[row * a.G + grp] & 15u;
+                continue;
+            }
+            const int k1 = min((int64_t)a.K, ((int64_t)grp + 1) * a.group);
+            float lo = 0.0f, hi = 0.0f;
+            for (int k = grp * a.group + lane; k < k1; k += 32) {
+                const float v = load_as(a.w, row * a.K + k, a.w_type);
+                lo = fmaxf(lo, -v);
+                hi = fmaxf(hi, v);
+            }
+            lo = warp_max(lo);
+            hi = warp_max(hi);
+            const float s = a.zeros ? (hi + lo) / 15.0f : fmaxf(hi, lo) / 7.0f;
+            float sr;
+            if (a.scale_bf16) {
+                const __nv_bfloat16 b = __float2bfloat16_rn(fminf(s, 3.3895313892515355e38f));
+                s2[h] = __bfloat16_as_ushort(b);
+                sr = __bfloat162float(b);
+            } else {
+                const __half b = __float2half_rn(fminf(s, 65504.0f));
+                s2[h] = __half_as_ushort(b);
+                sr = __half2float(b);
+            }
+            if (a.zeros && sr > 0.0f) z2[h] = (uint32_t)fminf(fmaxf(rintf(lo / sr), 0.0f), 15.0f);
+        }
+        const int size = 128 / a.sums;
+        const int64_t c1 = min((int64_t)a.Kp, ((int64_t)grp + 1) * a.group) / size;
+        for (int64_t c = (int64_t)grp * a.group / size + lane; c < c1; c += 32) {
+            const int64_t i = scale_index(a, et, g, (int)c);
+            reinterpret_cast<uint32_t*>(a.scales)[i] = s2[0] | s2[1] << 16;
+            if (a.zeros) a.zeros[i] = (uint8_t)(z2[0] | z2[1] << 4);
+        }
+    }
+}
+
+// one thread: a word, rows g and g + 8 x four consecutive inputs (behind gs4_scales_kernel)
+__global__ void __launch_bounds__(kThreads) gs4_codes_kernel(const PackArgs a)
+{
+    const int64_t words = (int64_t)a.E * a.tiles * (a.Kp / 64) * 128;
+    for (int64_t it = (int64_t)blockIdx.x * kThreads + threadIdx.x; it < words; it += (int64_t)gridDim.x * kThreads) {
+        const int w = (int)(it & 3), lane = (int)(it >> 2) & 31;
+        const int64_t blk = it >> 7;
+        const int kb = (int)(blk % (a.Kp / 64));
+        const int64_t et = blk / (a.Kp / 64);
+        const int64_t e = et / a.tiles;
+        const int m0 = (int)(et % a.tiles) * 16 + (lane >> 2);
+        const int k0 = kb * 64 + (w >> 1) * 32 + (lane & 3) * 8 + (w & 1) * 4;
+        const int64_t si = scale_index(a, et, lane >> 2, k0 / (128 / a.sums));
+        const uint32_t pair = reinterpret_cast<const uint32_t*>(a.scales)[si];
+        const uint32_t zz = a.zeros ? a.zeros[si] : 0x88u;
+        uint32_t out = 0;
+        for (int h = 0; h < 2; ++h) {
+            const int m = m0 + 8 * h;
+            const uint32_t z = (zz >> (4 * h)) & 15u;
+            const float s = scale_value((pair >> (16 * h)) & 0xffffu, a.scale_bf16);
+            for (int i = 0; i < 4; ++i) {
+                uint32_t u = z;                                            // beyond the matrix: zero
+                if (m < a.M && k0 + i < a.K) {
+                    const int64_t at = (e * a.M + m) * a.K + k0 + i;
+                    if (!a.w) {
+                        u = a.codes_in[at] & 15u;
+                    } else if (s > 0.0f) {
+                        const float q = rintf(load_as(a.w, at, a.w_type) / s);
+                        u = a.zeros ? (uint32_t)fminf(fmaxf(q + (float)z, 0.0f), 15.0f) : (uint32_t)(8.0f + fminf(fmaxf(q, -7.0f), 7.0f));
+                    }
+                }
+                out |= u << (4 * ((i >> 1) * 2 + h + 4 * (i & 1)));
+            }
+        }
+        reinterpret_cast<uint32_t*>(a.codes)[it] = out;
+    }
+}
+
+__global__ void __launch_bounds__(kThreads) gs4_unpack_kernel(const PackArgs a, uint8_t* codes, uint16_t* scale, uint8_t* zero)
+{
+    const int64_t count = (int64_t)a.E * a.M * a.K;
+    for (int64_t it = (int64_t)blockIdx.x * kThreads + threadIdx.x; it < count; it += (int64_t)gridDim.x * kThreads) {
+        const int k = (int)(it % a.K);
+        const int64_t row = it / a.K;
+        const int m = (int)(row % a.M);
+        const int64_t et = row / a.M * a.tiles + m / 16;
+        const int g = m & 7, h = (m >> 3) & 1, o = k & 31, i = o & 3;
+        const int64_t word = ((et * (a.Kp / 64) + k / 64) * 32 + g * 4 + (o >> 3)) * 4 + ((k >> 5) & 1) * 2 + ((o >> 2) & 1);
+        codes[it] = (uint8_t)(reinterpret_cast<const uint32_t*>(a.codes)[word] >> (4 * ((i >> 1) * 2 + h + 4 * (i & 1))) & 15u);
+        if (k % a.group == 0) {
+            const int64_t si = scale_index(a, et, g, k / (128 / a.sums));
+            const int64_t to = row * a.G + k / a.group;
+            if (scale) scale[to] = (uint16_t)(reinterpret_cast<const uint32_t*>(a.scales)[si] >> (16 * h));
+            if (zero) zero[to] = a.zeros ? (uint8_t)(a.zeros[si] >> (4 * h) & 15u) : (uint8_t)8;
+        }
+    }
+}
+
+struct HeaderWords { uint32_t w[8]; };
+__global__ void gs4_header_kernel(uint32_t* blob, const HeaderWords h)
+{
+    // (the status word is among the zeros)
+    blob[threadIdx.x] = threadIdx.x < 8 ? h.w[threadIdx.x] : 0u;
+}
+
+PackArgs args_of(const rmsmp_gs4_layer& L, uint8_t* blob)
+{
+    PackArgs a = {};
+    a.codes = blob + L.off_codes; a.scales = blob + L.off_scales;
+    a.zeros = L.mode == RMSMP_GS4_ZERO ? blob + L.off_zeros : nullptr;
+    a.M = L.M; a.K = L.K; a.Kp = L.Kp; a.tiles = L.tiles; a.E = L.E; a.group = L.group; a.sums = L.sums;
+    a.scale_bf16 = L.scale_type == RMSMP_BF16;
+    a.G = (int)(((int64_t)L.K + L.group - 1) / L.group);
+    return a;
+}
+
+unsigned blocks_for(int64_t items, int per_block)
+{
+    return (unsigned)std::max<int64_t>(1, std::min<int64_t>((items + per_block - 1) / per_block, (int64_t)sm_count() * 32));
+}
+
+cudaError_t launch_all(const rmsmp_gs4_layer& L, const PackArgs& a, uint8_t* blob, cudaStream_t st)
+{
+    // scales behind the last group are zeros
+    cudaError_t e = cudaMemsetAsync(a.scales, 0, (size_t)(L.packed_bytes - L.off_scales), st);
+    if (e != cudaSuccess) return e;
+    HeaderWords h = {{kGs4Magic, 1u, (uint32_t)L.E, (uint32_t)L.M, (uint32_t)L.K, (uint32_t)L.group, (uint32_t)L.mode, (uint32_t)L.scale_type}};
+    gs4_header_kernel<<<1, 64, 0, st>>>(reinterpret_cast<uint32_t*>(blob), h);
+    gs4_scales_kernel<<<blocks_for((int64_t)a.E * a.tiles * 8 * a.G, kThreads / 32), kThreads, 0, st>>>(a);
+    gs4_codes_kernel<<<blocks_for((int64_t)a.E * a.tiles * (a.Kp / 64) * 128, kThreads), kThreads, 0, st>>>(a);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_gs4_quantize(const rmsmp_gs4_layer& L, const void* dW, int w_type, uint8_t* blob, cudaStream_t st)
+{
+    PackArgs a = args_of(L, blob);
+    a.w = dW; a.w_type = w_type;
+    return launch_all(L, a, blob, st);
+}
+
+cudaError_t launch_gs4_pack(const rmsmp_gs4_layer& L, const uint8_t* codes, const void* scale, const uint8_t* zero, uint8_t* blob, cudaStream_t st)
+{
+    PackArgs a = args_of(L, blob);
+    a.codes_in = codes; a.scale_in = scale; a.zero_in = zero;
+    return launch_all(L, a, blob, st);
+}
+
+cudaError_t launch_gs4_unpack(const rmsmp_gs4_layer& L, const uint8_t* blob, uint8_t* codes, void* scale, uint8_t* zero, cudaStream_t st)
+{
+    const PackArgs a = args_of(L, const_cast<uint8_t*>(blob));
+    gs4_unpack_kernel<<<blocks_for((int64_t)a.E * a.M * a.K, kThreads), kThreads, 0, st>>>(a, codes, static_cast<uint16_t*>(scale), zero);
+    return cudaGetLastError();
+}
+
+}  // namespace rmsmp

@@ -5,6 +5,7 @@
 #include <mutex>
 #include <vector>
 #include "common.cuh"
+#include "nvtx.cuh"
 
 using namespace rmsmp;
 
@@ -154,18 +155,9 @@ rmsmp_status dispatch(Problem& p, rmsmp_variant variant, cudaStream_t st)
 
 }  // namespace
 
-#include <nvtx3/nvToolsExt.h>
-
-// A named NVTX range around every call that queues GPU work: a profiler's timeline shows which API call a
-// kernel belongs to.  Without a tool attached the two calls return at once.
-struct NvtxRange {
-    explicit NvtxRange(const char* name) { nvtxRangePushA(name); }
-    ~NvtxRange() { nvtxRangePop(); }
-    NvtxRange(const NvtxRange&) = delete;
-    NvtxRange& operator=(const NvtxRange&) = delete;
-};
-
 namespace rmsmp {
+
+rmsmp_status arch_status() { return check_arch(); }
 
 int device_ordinal()
 {

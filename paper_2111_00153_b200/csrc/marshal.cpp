@@ -31,13 +31,22 @@ struct Api {
     decltype(&rmsmp_assign_quantize_pack) assign_quantize_pack;
     decltype(&rmsmp_quantize_pack) quantize_pack;
     decltype(&rmsmp_gemm_grouped_launch) gemm_grouped_launch;
+    decltype(&rmsmp_gs4_quantize_pack) gs4_quantize_pack;
+    decltype(&rmsmp_gs4_pack_codes) gs4_pack_codes;
+    decltype(&rmsmp_gs4_unpack) gs4_unpack;
+    decltype(&rmsmp_gs4_gemm) gs4_gemm;
+    decltype(&rmsmp_gs4_gemm_experts) gs4_gemm_experts;
+    decltype(&rmsmp_expert_sort) expert_sort;
+    decltype(&rmsmp_expert_gather) expert_gather;
+    decltype(&rmsmp_expert_combine) expert_combine;
+    decltype(&rmsmp_expert_combine_backward) expert_combine_backward;
 } api;
 
 PyObject* g_stream;          // callable: the current stream's handle
 PyObject *g_raw, *g_device;  // torch's accessors, once CUDA has been started up: g_raw(g_device()) is that handle
 PyObject* g_error;           // callable(status, where): raises RmsmpError
 PyObject* g_array;           // callable(object, format): a contiguous array of bytes ('B') or floats ('f') with its values
-PyObject *s_data_ptr, *s_numel, *s_element_size, *s_cuda_stream;
+PyObject *s_data_ptr, *s_numel, *s_element_size, *s_cuda_stream, *s_get_device;
 
 // Arguments of one call, positions filled from positional and keyword arguments; conversions record the first failure.
 struct Call {
@@ -120,6 +129,32 @@ struct Call {
         void* p = address(r);
         Py_DECREF(r);
         return p;
+    }
+    // The same for calls that say so when a tensor is not on the current device: a kernel that is given host memory, or another
+    // GPU's, would fault.  (An int is taken as it is.)  `size`: bytes of its elements, where they can be only one.
+    long long device = -2;                                      // current device, once asked for
+    void* here(int i, long size = 0)
+    {
+        if (!ok || none(i) || PyLong_Check(a[i])) return ptr(i);
+        if (device == -2 && g_device) device = number(PyObject_CallNoArgs(g_device));
+        const long long on = number(PyObject_CallMethodNoArgs(a[i], s_get_device));
+        const long long bytes = size ? number(PyObject_CallMethodNoArgs(a[i], s_element_size)) : 0;
+        if (ok && (on < 0 || (device >= 0 && on != device))) {
+            PyErr_SetString(PyExc_ValueError, on < 0 ? "a tensor is not on a CUDA device" : "a tensor is not on the current CUDA device");
+            ok = false;
+        } else if (ok && bytes != size) {
+            PyErr_Format(PyExc_ValueError, "argument %d needs elements of %ld bytes (%lld given)", i, size, bytes);
+            ok = false;
+        }
+        return ptr(i);
+    }
+    long long number(PyObject* r)                               // what a method returned
+    {
+        if (!r) { ok = false; return -1; }
+        const long long v = PyLong_AsLongLong(r);
+        Py_DECREF(r);
+        if (v == -1 && PyErr_Occurred()) ok = false;
+        return v;
     }
     size_t bytes_of(int i)                                      // numel() * element_size() of a tensor
     {
@@ -457,6 +492,135 @@ DEF(gemm_grouped_launch)
     Py_RETURN_NONE;
 }
 
+DEF(gs4_quantize_pack)
+{
+    ARGS("rmsmp_gs4_quantize_pack", 4, "layer", "d_W", "w_type", "d_packed", "packed_bytes", "stream")
+    void* s = c.stream(5);
+    const rmsmp_gs4_layer* L = c.structure<rmsmp_gs4_layer>(0);
+    void* W = c.here(1);
+    const int type = c.i32(2);
+    void* pk = c.here(3);
+    const size_t bytes = c.none(4) ? c.bytes_of(3) : c.size(4);
+    RUN("rmsmp_gs4_quantize_pack", api.gs4_quantize_pack(L, W, (rmsmp_dtype)type, pk, bytes, s))
+    Py_RETURN_NONE;
+}
+
+DEF(gs4_pack_codes)
+{
+    ARGS("rmsmp_gs4_pack_codes", 5, "layer", "d_codes", "d_scale", "d_zero", "d_packed", "packed_bytes", "stream")
+    void* s = c.stream(6);
+    const rmsmp_gs4_layer* L = c.structure<rmsmp_gs4_layer>(0);
+    void *codes = c.here(1, 1), *scale = c.here(2, 2), *zero = c.here(3, 1), *pk = c.here(4);
+    const size_t bytes = c.none(5) ? c.bytes_of(4) : c.size(5);
+    RUN("rmsmp_gs4_pack_codes", api.gs4_pack_codes(L, (const uint8_t*)codes, scale, (const uint8_t*)zero, pk, bytes, s))
+    Py_RETURN_NONE;
+}
+
+DEF(gs4_unpack)
+{
+    ARGS("rmsmp_gs4_unpack", 3, "layer", "d_packed", "d_codes", "d_scale", "d_zero", "stream")
+    void* s = c.stream(5);
+    const rmsmp_gs4_layer* L = c.structure<rmsmp_gs4_layer>(0);
+    void *pk = c.here(1), *codes = c.here(2, 1), *scale = c.here(3, 2), *zero = c.here(4, 1);
+    RUN("rmsmp_gs4_unpack", api.gs4_unpack(L, pk, (uint8_t*)codes, scale, (uint8_t*)zero, s))
+    Py_RETURN_NONE;
+}
+
+DEF(gs4_gemm)
+{
+    ARGS("rmsmp_gs4_gemm", 9, "layer", "d_packed", "d_x", "x_type", "N", "ld_x", "d_y", "y_type", "ld_y", "stream")
+    void* s = c.stream(9);
+    const rmsmp_gs4_layer* L = c.structure<rmsmp_gs4_layer>(0);
+    void *pk = c.here(1), *x = c.here(2);
+    const int x_type = c.i32(3);
+    const long long N = c.i64(4), ld_x = c.i64(5);
+    void* y = c.here(6);
+    const int y_type = c.i32(7);
+    const long long ld_y = c.i64(8);
+    RUN("rmsmp_gs4_gemm", api.gs4_gemm(L, pk, x, (rmsmp_dtype)x_type, N, ld_x, y, (rmsmp_dtype)y_type, ld_y, s))
+    Py_RETURN_NONE;
+}
+
+DEF(gs4_gemm_experts)
+{
+    ARGS("rmsmp_gs4_gemm_experts", 12, "layer", "d_packed", "d_x", "x_type", "x_rows", "ld_x", "d_rows", "d_offsets", "R", "d_y", "y_type", "ld_y", "stream")
+    void* s = c.stream(12);
+    const rmsmp_gs4_layer* L = c.structure<rmsmp_gs4_layer>(0);
+    void *pk = c.here(1), *x = c.here(2);
+    const int x_type = c.i32(3);
+    const long long x_rows = c.i64(4), ld_x = c.i64(5);
+    void *rows = c.here(6, 4), *offsets = c.here(7, 4);
+    const long long R = c.i64(8);
+    void* y = c.here(9);
+    const int y_type = c.i32(10);
+    const long long ld_y = c.i64(11);
+    RUN("rmsmp_gs4_gemm_experts", api.gs4_gemm_experts(L, pk, x, (rmsmp_dtype)x_type, x_rows, ld_x, (const int32_t*)rows, (const int32_t*)offsets, R, y,
+                                                       (rmsmp_dtype)y_type, ld_y, s))
+    Py_RETURN_NONE;
+}
+
+DEF(expert_sort)
+{
+    ARGS("rmsmp_expert_sort", 7, "d_ids", "T", "k", "E", "d_offsets", "d_rows", "d_place", "stream")
+    void* s = c.stream(7);
+    void* ids = c.here(0, 4);
+    const long long T = c.i64(1);
+    const int k = c.i32(2), E = c.i32(3);
+    void *offsets = c.here(4, 4), *rows = c.here(5, 4), *place = c.here(6, 4);
+    RUN("rmsmp_expert_sort", api.expert_sort((const int32_t*)ids, T, k, E, (int32_t*)offsets, (int32_t*)rows, (int32_t*)place, s))
+    Py_RETURN_NONE;
+}
+
+DEF(expert_gather)
+{
+    ARGS("rmsmp_expert_gather", 9, "d_x", "type", "x_rows", "H", "ld_x", "d_rows", "R", "d_xs", "ld_xs", "stream")
+    void* s = c.stream(9);
+    void* x = c.here(0);
+    const int type = c.i32(1);
+    const long long x_rows = c.i64(2), H = c.i64(3), ld_x = c.i64(4);
+    void* rows = c.here(5, 4);
+    const long long R = c.i64(6);
+    void* xs = c.here(7);
+    const long long ld_xs = c.i64(8);
+    RUN("rmsmp_expert_gather", api.expert_gather(x, (rmsmp_dtype)type, x_rows, H, ld_x, (const int32_t*)rows, R, xs, ld_xs, s))
+    Py_RETURN_NONE;
+}
+
+DEF(expert_combine)
+{
+    ARGS("rmsmp_expert_combine", 11, "d_ys", "type", "R", "H", "ld_ys", "d_place", "d_w", "T", "k", "d_y", "ld_y", "stream")
+    void* s = c.stream(11);
+    void* ys = c.here(0);
+    const int type = c.i32(1);
+    const long long R = c.i64(2), H = c.i64(3), ld_ys = c.i64(4);
+    void *place = c.here(5, 4), *w = c.here(6, 4);
+    const long long T = c.i64(7);
+    const int k = c.i32(8);
+    void* y = c.here(9);
+    const long long ld_y = c.i64(10);
+    RUN("rmsmp_expert_combine", api.expert_combine(ys, (rmsmp_dtype)type, R, H, ld_ys, (const int32_t*)place, (const float*)w, T, k, y, ld_y, s))
+    Py_RETURN_NONE;
+}
+
+DEF(expert_combine_backward)
+{
+    ARGS("rmsmp_expert_combine_backward", 14, "d_dy", "type", "T", "k", "H", "ld_dy", "d_ys", "R", "ld_ys", "d_place", "d_w", "d_dys", "ld_dys", "d_dw", "stream")
+    void* s = c.stream(14);
+    void* dy = c.here(0);
+    const int type = c.i32(1);
+    const long long T = c.i64(2);
+    const int k = c.i32(3);
+    const long long H = c.i64(4), ld_dy = c.i64(5);
+    void* ys = c.here(6);
+    const long long R = c.i64(7), ld_ys = c.i64(8);
+    void *place = c.here(9, 4), *w = c.here(10, 4), *dys = c.here(11);
+    const long long ld_dys = c.i64(12);
+    void* dw = c.here(13, 4);
+    RUN("rmsmp_expert_combine_backward", api.expert_combine_backward(dy, (rmsmp_dtype)type, T, k, H, ld_dy, ys, R, ld_ys, (const int32_t*)place, (const float*)w,
+                                                                     dys, ld_dys, (float*)dw, s))
+    Py_RETURN_NONE;
+}
+
 // setup(addresses: {name: int}, stream: callable, error: callable, array: callable)
 PyObject* setup(PyObject*, PyObject* args)
 {
@@ -477,7 +641,16 @@ PyObject* setup(PyObject*, PyObject* args)
         !get("rmsmp_conv_implicit_workspace_requant", api.conv_implicit_workspace_requant) || !get("rmsmp_conv_depthwise", api.conv_depthwise) ||
         !get("rmsmp_im2col_codes", api.im2col_codes) || !get("rmsmp_expand_weights", api.expand_weights) ||
         !get("rmsmp_assign_quantize_pack", api.assign_quantize_pack) || !get("rmsmp_gemm_grouped_launch", api.gemm_grouped_launch) ||
-        !get("rmsmp_quantize_pack", api.quantize_pack))
+        !get("rmsmp_quantize_pack", api.quantize_pack) ||
+        !get("rmsmp_gs4_quantize_pack", api.gs4_quantize_pack) ||
+        !get("rmsmp_gs4_pack_codes", api.gs4_pack_codes) ||
+        !get("rmsmp_gs4_unpack", api.gs4_unpack) ||
+        !get("rmsmp_gs4_gemm", api.gs4_gemm) ||
+        !get("rmsmp_gs4_gemm_experts", api.gs4_gemm_experts) ||
+        !get("rmsmp_expert_sort", api.expert_sort) ||
+        !get("rmsmp_expert_gather", api.expert_gather) ||
+        !get("rmsmp_expert_combine", api.expert_combine) ||
+        !get("rmsmp_expert_combine_backward", api.expert_combine_backward))
         return nullptr;
     Py_INCREF(stream); Py_XSETREF(g_stream, stream);
     Py_INCREF(error); Py_XSETREF(g_error, error);
@@ -513,6 +686,15 @@ PyMethodDef methods[] = {
     METHOD(assign_quantize_pack, "Row assignment on the device + quantize + pack, from the ratio alone."),
     METHOD(quantize_pack, "Quantize + group + pack by a given scheme, precision and scale per row."),
     METHOD(gemm_grouped_launch, "One launch of a prepared grouped plan."),
+    METHOD(gs4_quantize_pack, "Quantize + pack weights with a scale for every group of inputs."),
+    METHOD(gs4_pack_codes, "Pack codes, scales and zero points that are there already."),
+    METHOD(gs4_unpack, "The codes, scales and zero points of a packed layer."),
+    METHOD(gs4_gemm, "Linear layer of 4-bit weights with group scales."),
+    METHOD(gs4_gemm_experts, "The same for tokens sorted by expert."),
+    METHOD(expert_sort, "Tokens sorted by expert."),
+    METHOD(expert_gather, "Rows of tokens in sorted order."),
+    METHOD(expert_combine, "Weighted sums back to tokens."),
+    METHOD(expert_combine_backward, "The gradient of expert_combine."),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_marshal", "Argument marshalling of librmsmp's per-layer calls.", -1, methods, nullptr, nullptr, nullptr, nullptr};
@@ -525,5 +707,6 @@ PyMODINIT_FUNC PyInit__marshal(void)
     s_numel = PyUnicode_InternFromString("numel");
     s_element_size = PyUnicode_InternFromString("element_size");
     s_cuda_stream = PyUnicode_InternFromString("cuda_stream");
+    s_get_device = PyUnicode_InternFromString("get_device");
     return PyModule_Create(&module_def);
 }

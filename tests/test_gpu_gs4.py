@@ -1,0 +1,493 @@
+"""Group-scaled 4-bit layers and expert operators on the GPU against plain definitions in 64 bits.
+
+Tolerances.  A stored value is rounded once to its type: half a step, eps / 2 of the value.  In front of that stand fp32 sums.  A term of a
+product passes at most 16 additions inside a matrix instruction, 8 instructions of a sum over 128 inputs, one addition for every 128
+inputs, and 24 where warps, cluster and parts join, each off by at most 2^-23 (matrix instructions cut off) of the sum of the terms' magnitudes S:
+D * 2^-23 * S with D = 48 + K / 128.  (The scale's multiplication and the zero point are exact or one of these.)  A weighted sum back of k rows
+passes k additions, 2^-24 each; a dot product of H values by threads at most H / 16 + 24."""
+import numpy as np
+import pytest
+
+from oracle import gs4_oracle as G
+from paper_2111_00153_b200 import binding as R
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f32": R.F32, "f16": R.F16, "bf16": R.BF16}
+TINY = {"f32": 2.0 ** -149, "f16": 2.0 ** -24, "bf16": 2.0 ** -133}
+
+
+def td(name):
+    import torch
+    return {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}[name]
+
+
+def half_step(name):
+    import torch
+    return torch.finfo(td(name)).eps / 2
+
+
+def dev(a, name=None):
+    import torch
+    t = torch.from_numpy(np.ascontiguousarray(a)).cuda()
+    return t if name is None else t.to(td(name))
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+class Packed:
+    """A layer of random weights, packed from codes; `w`: [E][M][K] in 64 bits."""
+
+    def __init__(self, seed, E, M, K, group, mode, scale_type="bf16", spread=0.02):
+        import torch
+        rng = np.random.default_rng(seed)
+        Gn = -(-K // group)
+        self.codes = rng.integers(0, 16, (E, M, K)).astype(np.uint8)
+        scale = G.round_to((spread * (0.5 + rng.random((E, M, Gn)))).astype(np.float32), scale_type)
+        self.zero = rng.integers(0, 16, (E, M, Gn)).astype(np.uint8) if mode == R.GS4_ZERO else np.full((E, M, Gn), 8, np.uint8)
+        self.scale = scale
+        self.w = G.weights(self.codes, scale, self.zero, group)
+        self.layer = R.rmsmp_gs4_layer_init(E, M, K, group, mode, TYPES[scale_type])
+        self.buf = torch.full((self.layer.packed_bytes + 512,), 0xA5, dtype=torch.uint8, device="cuda")
+        self.packed = self.buf[256:-256]
+        R.rmsmp_gs4_pack_codes(self.layer, dev(self.codes), dev(scale, scale_type), dev(self.zero) if mode == R.GS4_ZERO else None, self.packed)
+
+
+def framed(rows, cols, ld, name, fill=float("nan")):
+    """A [rows][ld] output with spare rows and columns around it, all `fill`."""
+    import torch
+    buf = torch.full(((rows + 2) * ld + 64,), fill, dtype=td(name), device="cuda")
+    return buf, buf[ld + 32:ld + 32 + rows * ld].view(rows, ld)
+
+
+def check_close(y, ref, absum, name, depth, eps=2.0 ** -23):
+    fin = np.isfinite(ref)
+    err = np.abs(y - ref)
+    tol = half_step(name) * np.abs(ref) * (1 + 2.0 ** -10) + depth * eps * absum + TINY[name]
+    bad = fin & ~(err <= tol)
+    assert not bad.any(), (np.argwhere(bad)[:5], y[bad][:5], ref[bad][:5], tol[bad][:5])
+
+
+def run_linear(p, x, x_name, y_name, pad_x=0, pad_y=0):
+    """x: [N][K] numpy, rounded to the type here.  Returns (y, reference, sums of magnitudes); checks that nothing else was written."""
+    import torch
+    N, K, M = x.shape[0], p.layer.K, p.layer.M
+    xb, xv = framed(N, K, K + pad_x, x_name)          # NaN around and between the rows
+    xv[:, :K] = dev(x.astype(np.float32)).to(td(x_name))
+    yb, yv = framed(N, M, M + pad_y, y_name)
+    R.rmsmp_gs4_gemm(p.layer, p.packed, xv, TYPES[x_name], N, K + pad_x, yv, TYPES[y_name], M + pad_y)
+    torch.cuda.synchronize()
+    assert R.rmsmp_last_device_status(p.packed) == R.OK
+    out = host(yv[:, :M])
+    yv[:, :M] = float("nan")
+    assert torch.isnan(yb).all()
+    ref, absum = G.product(p.w[0], host(xv[:, :K]))
+    return out, ref, absum
+
+
+# ------------------------------------------------------------------ packing
+
+@pytest.mark.parametrize("E, M, K, group", [(1, 1, 1, 32), (1, 16, 128, 128), (2, 17, 129, 32), (1, 33, 300, 64), (3, 5, 100, 96), (1, 40, 700, 256), (2, 8, 70, 4096)])
+@pytest.mark.parametrize("mode", [R.GS4_SYM, R.GS4_ZERO])
+@pytest.mark.parametrize("scale_type", ["f16", "bf16"])
+def test_pack_and_unpack(E, M, K, group, mode, scale_type):
+    import torch
+    p = Packed(E + M + K, E, M, K, group, mode, scale_type)
+    codes = torch.empty((E, M, K), dtype=torch.uint8, device="cuda")
+    scale = torch.empty(p.scale.shape, dtype=td(scale_type), device="cuda")
+    zero = torch.empty(p.zero.shape, dtype=torch.uint8, device="cuda")
+    R.rmsmp_gs4_unpack(p.layer, p.packed, codes, scale, zero)
+    assert np.array_equal(codes.cpu().numpy(), p.codes) and np.array_equal(zero.cpu().numpy(), p.zero)
+    assert np.array_equal(host(scale), p.scale.astype(np.float64))
+    assert (p.buf[:256] == 0xA5).all() and (p.buf[-256:] == 0xA5).all()
+
+
+@pytest.mark.parametrize("M, K, group", [(1, 1, 32), (20, 200, 32), (33, 300, 64), (16, 257, 128), (5, 333, 512)])
+@pytest.mark.parametrize("mode", [R.GS4_SYM, R.GS4_ZERO])
+@pytest.mark.parametrize("scale_type", ["f16", "bf16"])
+@pytest.mark.parametrize("w_type", ["f32", "f16", "bf16"])
+def test_quantizer_bit_for_bit(M, K, group, mode, scale_type, w_type):
+    import torch
+    rng = np.random.default_rng(M + K)
+    W = rng.standard_normal((2, M, K)).astype(np.float32) * np.float32(0.02)
+    W[0, 0, :min(K, 40)] = 0                            # a group of zeros
+    W[1, 0] = np.abs(W[1, 0])                           # one-sided rows
+    W[1, M - 1] = -np.abs(W[1, M - 1])
+    if scale_type == "f16" and w_type == "f32":
+        W[0, M - 1, :32] *= np.float32(1e-9)            # a step that fp16 rounds to zero
+        W[1, M // 2, :32] *= np.float32(1e8)            # and one beyond its range
+    dW = dev(W, w_type)
+    L = R.rmsmp_gs4_layer_init(2, M, K, group, mode, TYPES[scale_type])
+    packed = torch.empty(L.packed_bytes, dtype=torch.uint8, device="cuda")
+    R.rmsmp_gs4_quantize_pack(L, dW, TYPES[w_type], packed)
+    want = G.quantize(dW.float().cpu().numpy(), group, mode, scale_type)
+    codes = torch.empty((2, M, K), dtype=torch.uint8, device="cuda")
+    scale = torch.empty(want[1].shape, dtype=td(scale_type), device="cuda")
+    zero = torch.empty(want[2].shape, dtype=torch.uint8, device="cuda")
+    R.rmsmp_gs4_unpack(L, packed, codes, scale, zero)
+    assert np.array_equal(scale.float().cpu().numpy(), want[1])
+    assert np.array_equal(zero.cpu().numpy(), want[2])
+    assert np.array_equal(codes.cpu().numpy(), want[0])
+
+
+# ------------------------------------------------------------------ linear
+
+@pytest.mark.parametrize("N", [1, 2, 3, 5, 8, 9, 16, 17, 33, 70])
+@pytest.mark.parametrize("M, K, group", [(1, 1, 32), (16, 128, 128), (15, 31, 32), (130, 300, 64), (100, 1029, 96), (257, 640, 128)])
+@pytest.mark.parametrize("x_name", ["f32", "f16", "bf16"])
+def test_linear(N, M, K, group, x_name):
+    p = Packed(N * M + K, 1, M, K, group, R.GS4_ZERO if (N + M) & 1 else R.GS4_SYM, "f16" if K & 1 else "bf16")
+    x = np.random.default_rng(N + K).standard_normal((N, K))
+    y, ref, absum = run_linear(p, x, x_name, x_name)
+    check_close(y, ref, absum, x_name, 48 + K / 128)
+
+
+@pytest.mark.parametrize("x_name", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("y_name", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("mode", [R.GS4_SYM, R.GS4_ZERO])
+@pytest.mark.parametrize("N, pad_x, pad_y", [(1, 0, 0), (4, 8, 8), (7, 3, 1), (40, 5, 16)])
+def test_types_and_strides(x_name, y_name, mode, N, pad_x, pad_y):
+    p = Packed(N, 1, 75, 424, 64, mode, "f16")
+    x = np.random.default_rng(N).standard_normal((N, 424))
+    y, ref, absum = run_linear(p, x, x_name, y_name, pad_x, pad_y)
+    check_close(y, ref, absum, y_name, 52)
+
+
+@pytest.mark.parametrize("group", [32, 64, 96, 128, 256, 1 << 20])
+@pytest.mark.parametrize("K", [32, 127, 129, 1000])
+@pytest.mark.parametrize("mode", [R.GS4_SYM, R.GS4_ZERO])
+def test_groups(group, K, mode):
+    p = Packed(K, 1, 50, K, group, mode)
+    for N, name in ((1, "bf16"), (6, "f32"), (20, "f16")):
+        x = np.random.default_rng(K).standard_normal((N, K))
+        y, ref, absum = run_linear(p, x, name, name)
+        check_close(y, ref, absum, name, 48 + K / 128)
+
+
+@pytest.mark.parametrize("M, K, N", [(16, 20000, 1), (64, 9000, 33), (5000, 64, 2), (2500, 2500, 12), (48, 30011, 3), (300, 4096, 200)])
+@pytest.mark.parametrize("x_name", ["f32", "bf16"])
+def test_long_rows_and_many_rows(M, K, N, x_name):
+    p = Packed(M, 1, M, K, 128 if K % 2 == 0 else 32, R.GS4_ZERO)
+    x = np.random.default_rng(K).standard_normal((N, K))
+    y, ref, absum = run_linear(p, x, x_name, x_name)
+    check_close(y, ref, absum, x_name, 48 + K / 128)
+
+
+def test_no_tokens():
+    import torch
+    p = Packed(1, 1, 20, 40, 32, R.GS4_SYM)
+    R.rmsmp_gs4_gemm(p.layer, p.packed, None, R.F32, 0, 40, None, R.F32, 20)
+    torch.cuda.synchronize()
+
+
+def test_exact_where_everything_is_small_integers():
+    """Scales of one and whole activations: every sum is a whole number below 2^24, so the result is exact in fp32."""
+    for x_name in ("f32", "f16", "bf16"):
+        rng = np.random.default_rng(5)
+        p = Packed(7, 1, 65, 515, 64, R.GS4_ZERO)
+        p2 = Packed(7, 1, 65, 515, 64, R.GS4_ZERO, spread=0.0)
+        import torch
+        R.rmsmp_gs4_pack_codes(p2.layer, dev(p.codes), dev(np.ones(p.scale.shape, np.float32), "bf16"), dev(p.zero), p2.packed)
+        p2.w = G.weights(p.codes, np.ones(p.scale.shape), p.zero, 64)
+        x = rng.integers(-9, 10, (11, 515)).astype(np.float64)
+        y, ref, _ = run_linear(p2, x, x_name, "f32")
+        assert np.array_equal(y, ref)
+
+
+@pytest.mark.parametrize("x_name", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("N", [1, 4, 20])
+def test_infinities_and_nans_stay_in_their_rows(x_name, N):
+    p = Packed(3, 1, 40, 200, 32, R.GS4_SYM)
+    x = np.random.default_rng(3).standard_normal((N + 3, 200))
+    x[0, 5] = np.inf
+    x[1, 100] = -np.inf
+    x[2, 199] = np.nan
+    import torch
+    dx = dev(x.astype(np.float32)).to(td(x_name))
+    y = torch.empty((N + 3, 40), dtype=td(x_name), device="cuda")
+    R.rmsmp_gs4_gemm(p.layer, p.packed, dx, TYPES[x_name], N + 3, 200, y, TYPES[x_name], 40)
+    out = host(y)
+    with np.errstate(invalid="ignore"):
+        ref = host(dx) @ p.w[0].T
+    assert np.array_equal(np.isnan(out[:3]), np.isnan(ref[:3]))
+    fin = ~np.isnan(ref[:3])
+    assert np.array_equal(out[:3][fin], ref[:3][fin])
+    r, a = G.product(p.w[0], host(dx)[3:])
+    check_close(out[3:], r, a, x_name, 52)
+
+
+def test_fp32_activations_over_their_whole_range():
+    """The largest and the smallest normal numbers: parts are cut off, not rounded, so none overflows."""
+    p = Packed(9, 1, 20, 96, 32, R.GS4_SYM, spread=0.001)
+    for size in (3.4e38, 1e-30, 2.0 ** -126):
+        x = np.sign(np.random.default_rng(1).standard_normal((2, 96))) * 0
+        x[0, 3] = size
+        x[1, 90] = -size
+        y, ref, absum = run_linear(p, x, "f32", "f32")
+        if size == 3.4e38:
+            big = np.abs(ref / p.scale[0, :, [0]][0, 0]) < 1e38         # the sum of codes times activations has to fit
+            code = p.codes[0].astype(np.int64) - 8
+            fits = np.stack([np.abs(code[:, 3]) <= 1, np.abs(code[:, 90]) <= 1])
+            y, ref, absum = y[fits], ref[fits], absum[fits]
+        tol = 2.0 ** -23 * np.abs(ref) * 4 + 2.0 ** -126 * 2.0 ** -10
+        assert np.all(np.abs(y - ref) <= tol)
+
+
+# ------------------------------------------------------------------ experts
+
+def route(seed, T, k, E, padded=0.0, only=None):
+    rng = np.random.default_rng(seed)
+    ids = np.stack([rng.permutation(E)[:k] if k <= E else rng.integers(0, E, k) for _ in range(T)]) if T else np.zeros((0, k))
+    if only is not None:
+        ids = rng.choice(only, (T, k))
+    ids[rng.random(T) < padded] = -1
+    return ids.astype(np.int32)
+
+
+@pytest.mark.parametrize("T, k, E, kind", [(1, 1, 1, "all"), (1, 2, 8, "all"), (5, 2, 4, "padded"), (40, 3, 7, "all"), (64, 2, 3, "padded"), (9, 2, 6, "none"),
+                                           (70, 1, 5, "one"), (300, 4, 16, "padded"), (3, 8, 100, "all")])
+@pytest.mark.parametrize("x_name", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("by_rows", [True, False])
+def test_experts(T, k, E, kind, x_name, by_rows):
+    import torch
+    M, K = 50, 200
+    p = Packed(T + E, E, M, K, 64, R.GS4_ZERO if E & 1 else R.GS4_SYM)
+    ids = route(T, T, k, E, {"padded": 0.3, "none": 1.0}.get(kind, 0.0), [E // 2] if kind == "one" else None)
+    offsets, rows, _ = G.sort_pairs(ids, E)
+    x = np.random.default_rng(T).standard_normal((T, K))
+    dx = dev(x.astype(np.float32)).to(td(x_name))
+    dxs = dx if by_rows else dx[dev(np.maximum(rows, 0)).long()]
+    P = T * k
+    yb, y = framed(P, M, M + 3, x_name)
+    R.rmsmp_gs4_gemm_experts(p.layer, p.packed, dxs, TYPES[x_name], dxs.shape[0], K, dev(rows) if by_rows else None, dev(offsets), P, y, TYPES[x_name], M + 3)
+    torch.cuda.synchronize()
+    assert R.rmsmp_last_device_status(p.packed) == R.OK
+    out, hx = host(y), host(dx)
+    for e in range(E):
+        a, b = offsets[e], offsets[e + 1]
+        if b > a:
+            ref, absum = G.product(p.w[e], hx[rows[a:b]])
+            check_close(out[a:b, :M], ref, absum, x_name, 52)
+    y[:offsets[-1], :M] = float("nan")
+    assert torch.isnan(yb).all()                       # rows behind the last, and everything around, are as they were
+
+
+def test_experts_with_bad_offsets_and_rows_stay_inside():
+    """Offsets beyond the capacity are cut; a row index outside x is a row of zeros; falling offsets fault nothing."""
+    import torch
+    E, M, K, Rn = 4, 40, 96, 12
+    p = Packed(1, E, M, K, 32, R.GS4_SYM)
+    x = np.random.default_rng(1).standard_normal((5, K)).astype(np.float32)
+    rows = np.array([0, 4, 5, -1, 2, 1 << 30, -(1 << 31), 3, 1, 0, 0, 4], np.int32)
+    for offsets in ([-7, 3, 3, 10, 99], [0, 5, 2, 2, 12], [12, 12, 12, 12, 40], [0, 0, 0, 0, 0]):
+        yb, y = framed(Rn, M, M, "f32")
+        R.rmsmp_gs4_gemm_experts(p.layer, p.packed, dev(x), R.F32, 5, K, dev(rows), dev(np.array(offsets, np.int32)), Rn, y, R.F32, M)
+        torch.cuda.synchronize()
+        out = host(y)
+        claims = [[] for _ in range(Rn)]
+        for e in range(E):
+            for q in range(max(0, offsets[e]), min(Rn, offsets[e + 1])):
+                claims[q].append(e)
+        for q, of in enumerate(claims):
+            xr = x[rows[q]].astype(np.float64) if 0 <= rows[q] < 5 else np.zeros(K)
+            refs = [G.product(p.w[e], xr[None]) for e in of]
+            if len(of) == 1:
+                check_close(out[q:q + 1], *refs[0], "f32", 52)
+            elif of:                                   # falling offsets, which the call does not allow, name a row twice: either's values
+                assert all(any(abs(out[q, m] - r[0, m]) <= 1e-4 * a[0, m] for r, a in refs) for m in range(M))
+        written = np.array([bool(of) for of in claims])
+        y[torch.from_numpy(written).cuda()] = float("nan")
+        assert torch.isnan(yb).all()
+
+
+# ------------------------------------------------------------------ order
+
+@pytest.mark.parametrize("T, k, E", [(0, 2, 8), (1, 1, 1), (1, 2, 8), (7, 3, 5), (33, 1, 2), (100, 8, 64), (1000, 2, 1024), (3000, 4, 17), (20000, 8, 256), (5, 1024, 3), (70001, 1, 33)])
+@pytest.mark.parametrize("kind", ["all", "padded", "none", "one", "wild"])
+def test_sort(T, k, E, kind):
+    import torch
+    rng = np.random.default_rng(T + k)
+    ids = rng.integers(0, E, (T, k)).astype(np.int32)
+    if kind == "padded":
+        ids[rng.random((T, k)) < 0.3] = -1
+    elif kind == "none":
+        ids[:] = E
+    elif kind == "one":
+        ids[:] = E - 1
+    elif kind == "wild":
+        ids = rng.integers(-2 ** 31, 2 ** 31, (T, k)).astype(np.int32)
+        ids[rng.random((T, k)) < 0.5] = 0
+    off = torch.full((E + 3,), -9, dtype=torch.int32, device="cuda")
+    rows = torch.full((T * k + 2,), -9, dtype=torch.int32, device="cuda")
+    place = torch.full((T * k + 2,), -9, dtype=torch.int32, device="cuda")
+    R.rmsmp_expert_sort(dev(ids), T, k, E, off[1:], rows[1:], place[1:])
+    want = G.sort_pairs(ids, E)
+    assert np.array_equal(off[1:E + 2].cpu().numpy(), want[0])
+    assert np.array_equal(rows[1:-1].cpu().numpy(), want[1])
+    assert np.array_equal(place[1:-1].cpu().numpy().reshape(T, k), want[2])
+    assert all(int(t[0]) == -9 and int(t[-1]) == -9 for t in (off, rows, place))
+
+
+# ------------------------------------------------------------------ rows
+
+ROWS = [(1, 1, 3, 1, 0), (1, 2, 8, 1024, 0), (5, 4, 16, 777, 0), (30, 2, 4, 64, 8), (30, 2, 4, 64, 3), (200, 8, 32, 2048, 0), (9, 3, 5, 8200, 0), (17, 1, 2, 33, 5),
+        (60, 20, 50, 24, 0)]
+
+
+@pytest.mark.parametrize("T, k, E, H, pad", ROWS)
+@pytest.mark.parametrize("name", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("padded", [0.0, 0.4, 1.0])
+def test_gather_and_combine(T, k, E, H, pad, name, padded):
+    import torch
+    ids = route(T + H, T, k, E, padded)
+    offsets, rows, place = G.sort_pairs(ids, E)
+    P, kept = T * k, offsets[-1]
+    rng = np.random.default_rng(H)
+    xb, x = framed(T, H, H + pad, name)
+    x[:, :H] = dev(rng.standard_normal((T, H)).astype(np.float32)).to(td(name))
+    sb, xs = framed(P, H, H + pad, name)
+    R.rmsmp_expert_gather(x, TYPES[name], T, H, H + pad, dev(rows), P, xs, H + pad)
+    assert np.array_equal(host(xs[:kept, :H]), host(x[:, :H])[rows[:kept]])
+    keep = xs.clone()
+    xs[:kept, :H] = float("nan")
+    assert torch.isnan(sb).all()
+    w = rng.random((T, k)).astype(np.float32)
+    for weights in (w, None):
+        yb, y = framed(T, H, H + pad, name)
+        R.rmsmp_expert_combine(keep, TYPES[name], P, H, H + pad, dev(place), None if weights is None else dev(weights), T, k, y, H + pad)
+        ref, absum = G.combine(host(keep[:, :H]), place, weights)
+        check_close(host(y[:, :H]), ref, absum, name, k, 2.0 ** -24)
+        y[:, :H] = float("nan")
+        assert torch.isnan(yb).all()
+
+
+@pytest.mark.parametrize("T, k, E, H, pad", ROWS)
+@pytest.mark.parametrize("name", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("padded", [0.0, 0.4, 1.0])
+def test_combine_backward(T, k, E, H, pad, name, padded):
+    import torch
+    ids = route(T + H, T, k, E, padded)
+    _, _, place = G.sort_pairs(ids, E)
+    P = T * k
+    rng = np.random.default_rng(H + 1)
+    fill = lambda rows: dev(rng.standard_normal((rows, H)).astype(np.float32)).to(td(name))
+    _, dy = framed(T, H, H + pad, name)
+    _, ys = framed(P, H, H + pad, name)
+    dy[:, :H], ys[:, :H] = fill(T), fill(P)
+    w = rng.random((T, k)).astype(np.float32)
+    for weights in (w, None):
+        ref, dw_ref, absum = G.combine_backward(host(dy[:, :H]), host(ys[:, :H]), place, weights)
+        for want_dys, want_dw in ((True, True), (True, False), (False, True)):
+            sb, dys = framed(P, H, H + pad, name)
+            dwb = torch.full((T * k + 2,), -9.0, device="cuda")
+            R.rmsmp_expert_combine_backward(dy, TYPES[name], T, k, H, H + pad, ys if want_dw else None, P, H + pad, dev(place),
+                                            None if weights is None else dev(weights), dys if want_dys else None, H + pad, dwb[1:] if want_dw else None)
+            if want_dys:
+                out, kept = host(dys[:, :H]), ~np.isnan(ref[:, 0])
+                assert np.isnan(out[~kept]).all()
+                check_close(out[kept], ref[kept], np.abs(ref[kept]), name, 1, 2.0 ** -24)
+                dys[:, :H] = float("nan")
+            assert torch.isnan(sb).all()
+            if want_dw:
+                check_close(host(dwb[1:-1]).reshape(T, k), dw_ref, absum, "f32", H / 16 + 24, 2.0 ** -24)
+            assert float(dwb[0]) == -9.0 and float(dwb[-1]) == -9.0
+
+
+def test_gradients_against_differences():
+    """The sum is linear in the rows and in the weights: differences of the call itself give its gradient up to rounding."""
+    import torch
+    T, k, E, H = 6, 2, 3, 16
+    ids = route(4, T, k, E, 0.2)
+    _, rows, place = G.sort_pairs(ids, E)
+    P = T * k
+    rng = np.random.default_rng(8)
+    ys, w, dy = rng.standard_normal((P, H)).astype(np.float32), rng.random((T, k)).astype(np.float32), rng.standard_normal((T, H)).astype(np.float32)
+
+    def loss(a, b):
+        y = torch.empty((T, H), device="cuda")
+        R.rmsmp_expert_combine(dev(a), R.F32, P, H, H, dev(place), dev(b), T, k, y, H)
+        return float((host(y) * dy).sum())
+    dys, dw = torch.zeros((P, H), device="cuda"), torch.empty((T, k), device="cuda")
+    R.rmsmp_expert_combine_backward(dev(dy), R.F32, T, k, H, H, dev(ys), P, H, dev(place), dev(w), dys, H, dw)
+    room = 64 * 2.0 ** -24 * (1 + np.abs(dy).max()) * H          # two sums of T * H fp32 values, one of which moved by one
+    for p in range(0, P, 3):
+        d = np.zeros_like(ys)
+        d[p, p % H] = 1
+        assert abs(loss(ys + d, w) - loss(ys, w) - float(dys[p, p % H])) < room
+    for t in range(T):
+        d = np.zeros_like(w)
+        d[t, t % k] = 1
+        assert abs(loss(ys, w + d) - loss(ys, w) - float(dw[t, t % k])) < room
+
+
+# ------------------------------------------------------------------ together
+
+@pytest.mark.parametrize("name", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("T", [1, 24])
+def test_a_layer_of_experts_as_it_is_used(name, T):
+    """Sort, first product by the sorted rows, activation, second product, weighted sum back; then once more from a captured graph with new inputs."""
+    import torch
+    E, k, K, F = 6, 2, 96, 160
+    up, down = Packed(1, E, F, K, 32, R.GS4_ZERO), Packed(2, E, K, F, 64, R.GS4_SYM)
+    P, t = T * k, TYPES[name]
+    x = torch.empty((T, K), dtype=td(name), device="cuda")
+    ids, w = torch.empty((T, k), dtype=torch.int32, device="cuda"), torch.empty((T, k), device="cuda")
+    off, rows = torch.empty(E + 1, dtype=torch.int32, device="cuda"), torch.empty(P, dtype=torch.int32, device="cuda")
+    place = torch.empty((T, k), dtype=torch.int32, device="cuda")
+    h, z, y = torch.zeros((P, F), dtype=td(name), device="cuda"), torch.zeros((P, K), dtype=td(name), device="cuda"), torch.empty((T, K), dtype=td(name), device="cuda")
+
+    def step():
+        R.rmsmp_expert_sort(ids, T, k, E, off, rows, place)
+        R.rmsmp_gs4_gemm_experts(up.layer, up.packed, x, t, T, K, rows, off, P, h, t, F)
+        h.relu_()
+        R.rmsmp_gs4_gemm_experts(down.layer, down.packed, h, t, P, F, None, off, P, z, t, K)
+        R.rmsmp_expert_combine(z, t, P, K, K, place, w, T, k, y, K)
+
+    def new_inputs(seed):
+        rng = np.random.default_rng(seed)
+        x.copy_(dev(rng.standard_normal((T, K)).astype(np.float32)))
+        ids.copy_(dev(route(seed, T, k, E, 0.2)))
+        w.copy_(dev(rng.random((T, k)).astype(np.float32)))
+
+    def check():
+        torch.cuda.synchronize()
+        hid, hx, hw = ids.cpu().numpy(), host(x), host(w)
+        ref = np.zeros((T, K))
+        size = np.zeros((T, K))
+        for a in range(T):
+            for j in range(k):
+                e = hid[a, j]
+                if e >= 0:
+                    hh, ha = G.product(up.w[e], hx[a:a + 1])
+                    zz, za = G.product(down.w[e], np.maximum(hh, 0))
+                    ref[a] += hw[a, j] * zz[0]
+                    size[a] += hw[a, j] * (np.abs(down.w[e]) @ (ha[0]))          # magnitudes carried through both products
+        # h, z and y are each rounded to the type; everything else is fp32
+        assert np.all(np.abs(host(y) - ref) <= 3 * half_step(name) * (size + np.abs(ref)) + 200 * 2.0 ** -23 * size + TINY[name])
+    new_inputs(1)
+    step()
+    check()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for seed in (2, 3):
+        new_inputs(seed)
+        graph.replay()
+        check()
+
+
+def test_results_repeat_bit_for_bit():
+    import torch
+    p = Packed(3, 1, 1024, 4096, 128, R.GS4_SYM)
+    x = dev(np.random.default_rng(1).standard_normal((3, 4096)).astype(np.float32))
+    ys = [torch.empty((3, 1024), device="cuda") for _ in range(4)]
+    for y in ys:
+        R.rmsmp_gs4_gemm(p.layer, p.packed, x, R.F32, 3, 4096, y, R.F32, 1024)
+    assert all(torch.equal(ys[0], y) for y in ys)
