@@ -453,17 +453,18 @@ rmsmp_status rmsmp_gemm_builtin_scratch(const rmsmp_layer* layer, const void* d_
  *   y[n][m] = sum_k s[m][k / group] * (u[m][k] - z[m][k / group]) * x[n][k],       u, z in 0..15
  * RMSMP_GS4_SYM has z = 8 everywhere (the Fixed-4 rows of Eq. 1, group by group); RMSMP_GS4_ZERO stores one per group.
  * A layer holds E matrices of M rows and K inputs: E = 1 is a plain linear layer, more are the experts of one layer.
- * Codes times activations are summed in fp32 over 32, 64 or 128 inputs (the largest of these that divides the group), each
- * such sum is multiplied by its scale, and those are summed in fp32; the result is rounded once, to y's type.  A sum of codes
- * times activations beyond fp32's range is infinite even where the scale would bring it back.  Nothing else is rounded: codes are exact in
- * fp16 and bf16, and an fp32 activation is multiplied as three bf16 numbers that add up to it.
+ * Codes times activations are summed in fp32 over runs of 32, 64 or 128 inputs (the longest of these that divides the group), each
+ * such sum is multiplied by its scale, and those are summed in fp32; the result is rounded once, to y's type.  The products are those of
+ * fp16 numbers, in which codes and fp16 activations are exact.  A bf16 or fp32 activation is first scaled by the power of two that takes the
+ * largest of its run to 2^14..2^15, and is then one fp16 number (bf16) or the sum of two (fp32): off by at most 2^-40 of that largest one,
+ * and, in fp32, 2^-24 of itself.  An fp16 activation is taken as it is, so its sum over a run is below 2^27.
  *
  * Packed buffer: 256-byte header (device status word at byte 64, see rmsmp_last_device_status), then
- *   codes   [E][ceil(M/16)][Kp/64][32][16] bytes, Kp = K rounded up to 128: lane 4g + c's 16 bytes of a block of 16 rows and
- *           64 inputs, as four words.  Word 2b + j holds rows g and g + 8, inputs 32b + 8c + 4j + i (i = 0..3): nibble
- *           (i / 2) * 2 + (row >= 8) + 4 * (i & 1).  Codes beyond K and M stand for zero.
- *   scales  [E][ceil(M/16)][Kp/128][8][n][2], n = 1, 2 or 4 sums for every 128 inputs: rows g and g + 8
- *   zeros   [E][ceil(M/16)][Kp/128][8][n] bytes (RMSMP_GS4_ZERO only): row g's in the low, row g + 8's in the high half
+ *   blocks [E][ceil(M/32)][Kp/128][block_bytes], Kp = K rounded up to 128: 32 rows and 128 inputs of a matrix each, with
+ *   codes   [2][2][32][16] bytes: of 16 rows and 64 inputs, lane 4g + c's 16 bytes as four words.  Word 2b + j holds rows g and g + 8, inputs
+ *           32b + 8c + 4j + i (i = 0..3): nibble (i / 2) * 2 + (row >= 8) + 4 * (i & 1).  Codes beyond K and M stand for zero.
+ *   scales  [8][sums][4], sums = 1, 2 or 4 runs in 128 inputs: rows g, g + 8, g + 16, g + 24
+ *   zeros   [8][sums] 16-bit words (RMSMP_GS4_ZERO only): those rows' in four bits each, the lowest first
  */
 typedef enum { RMSMP_F32 = 0, RMSMP_F16 = 1, RMSMP_BF16 = 2 } rmsmp_dtype;
 typedef enum { RMSMP_GS4_SYM = 0, RMSMP_GS4_ZERO = 1 } rmsmp_gs4_mode;
@@ -472,9 +473,11 @@ typedef struct rmsmp_gs4_layer {
     int32_t E, M, K;            /* matrices; rows and inputs of each */
     int32_t group;              /* consecutive inputs of a row that share a scale */
     int32_t mode, scale_type;   /* rmsmp_gs4_mode; RMSMP_F16 or RMSMP_BF16 */
-    int32_t Kp, tiles;          /* K rounded up to 128; ceil(M/16) */
-    int32_t sums;               /* sums for every 128 inputs: 1, 2 or 4 */
-    uint64_t off_codes, off_scales, off_zeros;
+    int32_t Kp, tiles;          /* K rounded up to 128; ceil(M/32) */
+    int32_t sums;               /* runs in 128 inputs: 1, 2 or 4 */
+    int32_t block_bytes;        /* of 32 rows and 128 inputs, a multiple of 16 */
+    int32_t reserved;
+    uint64_t off_blocks;
     uint64_t packed_bytes;      /* size the packed buffer must have */
 } rmsmp_gs4_layer;
 

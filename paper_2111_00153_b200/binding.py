@@ -79,7 +79,7 @@ class rmsmp_gs4_layer(C.Structure):
         ("magic", C.c_uint32),
         ("E", C.c_int32), ("M", C.c_int32), ("K", C.c_int32), ("group", C.c_int32),
         ("mode", C.c_int32), ("scale_type", C.c_int32), ("Kp", C.c_int32), ("tiles", C.c_int32), ("sums", C.c_int32),
-        ("off_codes", C.c_uint64), ("off_scales", C.c_uint64), ("off_zeros", C.c_uint64), ("packed_bytes", C.c_uint64),
+        ("block_bytes", C.c_int32), ("reserved", C.c_int32), ("off_blocks", C.c_uint64), ("packed_bytes", C.c_uint64),
     ]
 
 

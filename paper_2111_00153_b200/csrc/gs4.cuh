@@ -10,13 +10,15 @@ constexpr uint32_t kGs4Magic = 0x47533452u;      // "GS4R"
 
 // The product y[p] = W x[row(p)]; passed by value.
 struct Gs4Args {
-    const uint8_t *codes, *scales, *zeros;       // sections of the packed buffer; zeros null: 8 everywhere
+    const uint8_t* blocks;                       // of 32 rows and 128 inputs: codes, scales, zeros
     const void* x;
     void* y;
     const int32_t *rows, *offsets;               // null: row p itself; one matrix and all R rows
     uint32_t* status;
     int64_t x_rows, ld_x, ld_y, R;
     int M, K, Kp, tiles, E, sums;
+    int sms;                                     // of the device
+    int block_bytes, has_zeros;                  // (no zeros: 8 everywhere)
     int scale_bf16, x_type, y_type, x_vec;       // x_vec: rows of x are 16-byte aligned
 };
 
@@ -32,6 +34,8 @@ cudaError_t launch_expert_combine(const void* ys, int type, int64_t R, int64_t H
                                   void* y, int64_t ld_y, cudaStream_t st);
 cudaError_t launch_expert_combine_backward(const void* dy, int type, int64_t T, int k, int64_t H, int64_t ld_dy, const void* ys, int64_t R, int64_t ld_ys,
                                            const int32_t* place, const float* w, void* dys, int64_t ld_dys, float* dw, cudaStream_t st);
+
+constexpr int kCodeBytes = 2048;                  // of a block
 
 __host__ __device__ inline int dtype_size(int t) { return t == RMSMP_F32 ? 4 : 2; }
 

@@ -22,13 +22,12 @@ inline rmsmp_status done(cudaError_t e)
 void lay_out(rmsmp_gs4_layer* L)
 {
     L->Kp = (int32_t)up((uint64_t)L->K, 128);
-    L->tiles = (L->M + 15) / 16;
+    L->tiles = (L->M + 31) / 32;
     L->sums = L->group % 128 == 0 ? 1 : L->group % 64 == 0 ? 2 : 4;
-    const uint64_t blocks = (uint64_t)L->E * L->tiles * (L->Kp / 128);      // of 16 rows and 128 inputs
-    L->off_codes = 256;
-    L->off_scales = L->off_codes + blocks * 1024;
-    L->off_zeros = up(L->off_scales + blocks * 32 * L->sums, 256);
-    L->packed_bytes = up(L->off_zeros + (L->mode == RMSMP_GS4_ZERO ? blocks * 8 * L->sums : 0), 256);
+    L->block_bytes = kCodeBytes + 64 * L->sums + (L->mode == RMSMP_GS4_ZERO ? 16 * L->sums : 0);
+    L->reserved = 0;
+    L->off_blocks = 256;
+    L->packed_bytes = up(L->off_blocks + (uint64_t)L->E * L->tiles * (L->Kp / 128) * L->block_bytes, 256);
     L->magic = kGs4Magic;
 }
 
@@ -46,8 +45,8 @@ bool gs4_ok(const rmsmp_gs4_layer* L)
     if (L->scale_type != RMSMP_F16 && L->scale_type != RMSMP_BF16) return false;
     rmsmp_gs4_layer want = *L;
     lay_out(&want);
-    return want.Kp == L->Kp && want.tiles == L->tiles && want.sums == L->sums && want.off_codes == L->off_codes && want.off_scales == L->off_scales &&
-           want.off_zeros == L->off_zeros && want.packed_bytes == L->packed_bytes;
+    return want.Kp == L->Kp && want.tiles == L->tiles && want.sums == L->sums && want.block_bytes == L->block_bytes &&
+           want.off_blocks == L->off_blocks && want.packed_bytes == L->packed_bytes;
 }
 
 rmsmp_status product(const rmsmp_gs4_layer* L, const void* d_packed, const void* d_x, rmsmp_dtype x_type, int64_t x_rows, int64_t ld_x,
@@ -64,14 +63,14 @@ rmsmp_status product(const rmsmp_gs4_layer* L, const void* d_packed, const void*
     if (arch != RMSMP_OK || R == 0) return arch;
     const uint8_t* blob = static_cast<const uint8_t*>(d_packed);
     Gs4Args a = {};
-    a.codes = blob + L->off_codes; a.scales = blob + L->off_scales;
-    a.zeros = L->mode == RMSMP_GS4_ZERO ? blob + L->off_zeros : nullptr;
+    a.blocks = blob + L->off_blocks; a.block_bytes = L->block_bytes; a.has_zeros = L->mode == RMSMP_GS4_ZERO;
     a.status = reinterpret_cast<uint32_t*>(const_cast<uint8_t*>(blob) + kStatusOffset);
     a.x = d_x; a.y = d_y; a.rows = d_rows; a.offsets = d_offsets;
     a.x_rows = x_rows; a.ld_x = ld_x; a.ld_y = ld_y; a.R = R;
     a.M = L->M; a.K = L->K; a.Kp = L->Kp; a.tiles = L->tiles; a.E = L->E; a.sums = L->sums;
     a.scale_bf16 = L->scale_type == RMSMP_BF16; a.x_type = x_type; a.y_type = y_type;
     a.x_vec = aligned(d_x, 16) && ld_x * dtype_size(x_type) % 16 == 0;
+    a.sms = sm_count();
     return done(launch_gs4_product(a, static_cast<cudaStream_t>(stream)));
 }
 

@@ -16,13 +16,17 @@ struct PackArgs {
     const uint8_t* codes_in;     // codes, scales, zeros (pack)
     const void* scale_in;
     const uint8_t* zero_in;
-    uint8_t *codes, *scales, *zeros;
-    int M, K, Kp, tiles, E, group, sums, scale_bf16, w_type, G;
+    uint8_t* blocks;
+    int M, K, Kp, tiles, E, group, sums, scale_bf16, w_type, G, block_bytes, has_zeros;
 };
 
-__device__ __forceinline__ int64_t scale_index(const PackArgs& a, int64_t et, int g, int chunk)      // of the pair (rows g, g + 8)
+// The scales and zero points of rows g, g + 8, g + 16, g + 24 for run number `run` of a row.
+struct Quad { uint2* scale; uint16_t* zero; };
+__device__ __forceinline__ Quad quad_of(const PackArgs& a, int64_t et, int g, int run)
 {
-    return ((et * (a.Kp / 128) + chunk / a.sums) * 8 + g) * a.sums + chunk % a.sums;
+    uint8_t* b = a.blocks + (et * (a.Kp / 128) + run / a.sums) * a.block_bytes + kCodeBytes;
+    const int i = g * a.sums + run % a.sums;
+    return {reinterpret_cast<uint2*>(b) + i, reinterpret_cast<uint16_t*>(b + 64 * a.sums) + i};
 }
 
 __device__ __forceinline__ float warp_max(float v)
@@ -31,7 +35,7 @@ __device__ __forceinline__ float warp_max(float v)
     return v;
 }
 
-// one warp: rows g and g + 8 of a block of 16, one group
+// one warp: rows g, g + 8, g + 16, g + 24 of a block, one group
 __global__ void __launch_bounds__(kThreads) gs4_scales_kernel(const PackArgs a)
 {
     const int lane = threadIdx.x & 31;
@@ -41,15 +45,16 @@ __global__ void __launch_bounds__(kThreads) gs4_scales_kernel(const PackArgs a)
         const int g = (int)(it / a.G % 8);
         const int64_t et = it / a.G / 8;
         const int64_t e = et / a.tiles;
-        const int m0 = (int)(et % a.tiles) * 16 + g;
-        uint32_t s2[2] = {0, 0}, z2[2] = {0, 0};
-        for (int h = 0; h < 2; ++h) {
+        const int m0 = (int)(et % a.tiles) * 32 + g;
+        uint32_t s2[4] = {}, z2[4] = {};
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
             const int m = m0 + 8 * h;
             if (m >= a.M) continue;
             const int64_t row = e * a.M + m;
             if (!a.w) {
                 s2[h] = static_cast<const uint16_t*>(a.scale_in)[row * a.G + grp];
-                if (a.zeros) z2[h] = a.zero_in[row * a.G + grp] & 15u;
+                if (a.has_zeros) z2[h] = a.zero_in[row * a.G + grp] & 15u;
                 continue;
             }
             const int k1 = min((int64_t)a.K, ((int64_t)grp + 1) * a.group);
@@ -61,7 +66,7 @@ __global__ void __launch_bounds__(kThreads) gs4_scales_kernel(const PackArgs a)
             }
             lo = warp_max(lo);
             hi = warp_max(hi);
-            const float s = a.zeros ? (hi + lo) / 15.0f : fmaxf(hi, lo) / 7.0f;
+            const float s = a.has_zeros ? (hi + lo) / 15.0f : fmaxf(hi, lo) / 7.0f;
             float sr;
             if (a.scale_bf16) {
                 const __nv_bfloat16 b = __float2bfloat16_rn(fminf(s, 3.3895313892515355e38f));
@@ -72,14 +77,14 @@ __global__ void __launch_bounds__(kThreads) gs4_scales_kernel(const PackArgs a)
                 s2[h] = __half_as_ushort(b);
                 sr = __half2float(b);
             }
-            if (a.zeros && sr > 0.0f) z2[h] = (uint32_t)fminf(fmaxf(rintf(lo / sr), 0.0f), 15.0f);
+            if (a.has_zeros && sr > 0.0f) z2[h] = (uint32_t)fminf(fmaxf(rintf(lo / sr), 0.0f), 15.0f);
         }
         const int size = 128 / a.sums;
         const int64_t c1 = min((int64_t)a.Kp, ((int64_t)grp + 1) * a.group) / size;
         for (int64_t c = (int64_t)grp * a.group / size + lane; c < c1; c += 32) {
-            const int64_t i = scale_index(a, et, g, (int)c);
-            reinterpret_cast<uint32_t*>(a.scales)[i] = s2[0] | s2[1] << 16;
-            if (a.zeros) a.zeros[i] = (uint8_t)(z2[0] | z2[1] << 4);
+            const Quad to = quad_of(a, et, g, (int)c);
+            *to.scale = make_uint2(s2[0] | s2[1] << 16, s2[2] | s2[3] << 16);
+            if (a.has_zeros) *to.zero = (uint16_t)(z2[0] | z2[1] << 4 | z2[2] << 8 | z2[3] << 12);
         }
     }
 }
@@ -87,18 +92,18 @@ __global__ void __launch_bounds__(kThreads) gs4_scales_kernel(const PackArgs a)
 // one thread: a word, rows g and g + 8 x four consecutive inputs (behind gs4_scales_kernel)
 __global__ void __launch_bounds__(kThreads) gs4_codes_kernel(const PackArgs a)
 {
-    const int64_t words = (int64_t)a.E * a.tiles * (a.Kp / 64) * 128;
+    const int64_t words = (int64_t)a.E * a.tiles * (a.Kp / 128) * 512;
     for (int64_t it = (int64_t)blockIdx.x * kThreads + threadIdx.x; it < words; it += (int64_t)gridDim.x * kThreads) {
-        const int w = (int)(it & 3), lane = (int)(it >> 2) & 31;
-        const int64_t blk = it >> 7;
-        const int kb = (int)(blk % (a.Kp / 64));
-        const int64_t et = blk / (a.Kp / 64);
+        const int w = (int)(it & 3), lane = (int)(it >> 2) & 31, part = (int)(it >> 7) & 1, half = (int)(it >> 8) & 1;
+        const int64_t blk = it >> 9;
+        const int kb = (int)(blk % (a.Kp / 128));
+        const int64_t et = blk / (a.Kp / 128);
         const int64_t e = et / a.tiles;
-        const int m0 = (int)(et % a.tiles) * 16 + (lane >> 2);
-        const int k0 = kb * 64 + (w >> 1) * 32 + (lane & 3) * 8 + (w & 1) * 4;
-        const int64_t si = scale_index(a, et, lane >> 2, k0 / (128 / a.sums));
-        const uint32_t pair = reinterpret_cast<const uint32_t*>(a.scales)[si];
-        const uint32_t zz = a.zeros ? a.zeros[si] : 0x88u;
+        const int m0 = (int)(et % a.tiles) * 32 + half * 16 + (lane >> 2);
+        const int k0 = kb * 128 + part * 64 + (w >> 1) * 32 + (lane & 3) * 8 + (w & 1) * 4;
+        const Quad of = quad_of(a, et, lane >> 2, k0 / (128 / a.sums));
+        const uint32_t pair = half ? of.scale->y : of.scale->x;
+        const uint32_t zz = a.has_zeros ? (uint32_t)*of.zero >> (8 * half) : 0x88u;
         uint32_t out = 0;
         for (int h = 0; h < 2; ++h) {
             const int m = m0 + 8 * h;
@@ -112,13 +117,13 @@ __global__ void __launch_bounds__(kThreads) gs4_codes_kernel(const PackArgs a)
                         u = a.codes_in[at] & 15u;
                     } else if (s > 0.0f) {
                         const float q = rintf(load_as(a.w, at, a.w_type) / s);
-                        u = a.zeros ? (uint32_t)fminf(fmaxf(q + (float)z, 0.0f), 15.0f) : (uint32_t)(8.0f + fminf(fmaxf(q, -7.0f), 7.0f));
+                        u = a.has_zeros ? (uint32_t)fminf(fmaxf(q + (float)z, 0.0f), 15.0f) : (uint32_t)(8.0f + fminf(fmaxf(q, -7.0f), 7.0f));
                     }
                 }
                 out |= u << (4 * ((i >> 1) * 2 + h + 4 * (i & 1)));
             }
         }
-        reinterpret_cast<uint32_t*>(a.codes)[it] = out;
+        reinterpret_cast<uint32_t*>(a.blocks + blk * a.block_bytes)[it & 511] = out;
     }
 }
 
@@ -129,31 +134,27 @@ __global__ void __launch_bounds__(kThreads) gs4_unpack_kernel(const PackArgs a, 
         const int k = (int)(it % a.K);
         const int64_t row = it / a.K;
         const int m = (int)(row % a.M);
-        const int64_t et = row / a.M * a.tiles + m / 16;
-        const int g = m & 7, h = (m >> 3) & 1, o = k & 31, i = o & 3;
-        const int64_t word = ((et * (a.Kp / 64) + k / 64) * 32 + g * 4 + (o >> 3)) * 4 + ((k >> 5) & 1) * 2 + ((o >> 2) & 1);
-        codes[it] = (uint8_t)(reinterpret_cast<const uint32_t*>(a.codes)[word] >> (4 * ((i >> 1) * 2 + h + 4 * (i & 1))) & 15u);
+        const int64_t et = row / a.M * a.tiles + m / 32;
+        const int g = m & 7, h = (m >> 3) & 1, quarter = (m >> 3) & 3, o = k & 31, i = o & 3;
+        const uint8_t* block = a.blocks + (et * (a.Kp / 128) + k / 128) * a.block_bytes;
+        const int word = ((((m >> 4) & 1) * 2 + ((k >> 6) & 1)) * 32 + g * 4 + (o >> 3)) * 4 + ((k >> 5) & 1) * 2 + ((o >> 2) & 1);
+        codes[it] = (uint8_t)(reinterpret_cast<const uint32_t*>(block)[word] >> (4 * ((i >> 1) * 2 + h + 4 * (i & 1))) & 15u);
         if (k % a.group == 0) {
-            const int64_t si = scale_index(a, et, g, k / (128 / a.sums));
+            const Quad of = quad_of(a, et, g, k / (128 / a.sums));
             const int64_t to = row * a.G + k / a.group;
-            if (scale) scale[to] = (uint16_t)(reinterpret_cast<const uint32_t*>(a.scales)[si] >> (16 * h));
-            if (zero) zero[to] = a.zeros ? (uint8_t)(a.zeros[si] >> (4 * h) & 15u) : (uint8_t)8;
+            if (scale) scale[to] = (uint16_t)((quarter & 2 ? of.scale->y : of.scale->x) >> (16 * (quarter & 1)));
+            if (zero) zero[to] = a.has_zeros ? (uint8_t)(*of.zero >> (4 * quarter) & 15u) : (uint8_t)8;
         }
     }
 }
 
 struct HeaderWords { uint32_t w[8]; };
-__global__ void gs4_header_kernel(uint32_t* blob, const HeaderWords h)
-{
-    // (the status word is among the zeros)
-    blob[threadIdx.x] = threadIdx.x < 8 ? h.w[threadIdx.x] : 0u;
-}
+__global__ void gs4_header_kernel(uint32_t* blob, const HeaderWords h) { blob[threadIdx.x] = h.w[threadIdx.x]; }
 
 PackArgs args_of(const rmsmp_gs4_layer& L, uint8_t* blob)
 {
     PackArgs a = {};
-    a.codes = blob + L.off_codes; a.scales = blob + L.off_scales;
-    a.zeros = L.mode == RMSMP_GS4_ZERO ? blob + L.off_zeros : nullptr;
+    a.blocks = blob + L.off_blocks; a.block_bytes = L.block_bytes; a.has_zeros = L.mode == RMSMP_GS4_ZERO;
     a.M = L.M; a.K = L.K; a.Kp = L.Kp; a.tiles = L.tiles; a.E = L.E; a.group = L.group; a.sums = L.sums;
     a.scale_bf16 = L.scale_type == RMSMP_BF16;
     a.G = (int)(((int64_t)L.K + L.group - 1) / L.group);
@@ -167,13 +168,13 @@ unsigned blocks_for(int64_t items, int per_block)
 
 cudaError_t launch_all(const rmsmp_gs4_layer& L, const PackArgs& a, uint8_t* blob, cudaStream_t st)
 {
-    // scales behind the last group are zeros
-    cudaError_t e = cudaMemsetAsync(a.scales, 0, (size_t)(L.packed_bytes - L.off_scales), st);
+    // the header's rest with its status word, and the scales behind a row's last group, are zeros
+    const cudaError_t e = cudaMemsetAsync(blob, 0, (size_t)L.packed_bytes, st);
     if (e != cudaSuccess) return e;
     HeaderWords h = {{kGs4Magic, 1u, (uint32_t)L.E, (uint32_t)L.M, (uint32_t)L.K, (uint32_t)L.group, (uint32_t)L.mode, (uint32_t)L.scale_type}};
-    gs4_header_kernel<<<1, 64, 0, st>>>(reinterpret_cast<uint32_t*>(blob), h);
+    gs4_header_kernel<<<1, 8, 0, st>>>(reinterpret_cast<uint32_t*>(blob), h);
     gs4_scales_kernel<<<blocks_for((int64_t)a.E * a.tiles * 8 * a.G, kThreads / 32), kThreads, 0, st>>>(a);
-    gs4_codes_kernel<<<blocks_for((int64_t)a.E * a.tiles * (a.Kp / 64) * 128, kThreads), kThreads, 0, st>>>(a);
+    gs4_codes_kernel<<<blocks_for((int64_t)a.E * a.tiles * (a.Kp / 128) * 512, kThreads), kThreads, 0, st>>>(a);
     return cudaGetLastError();
 }
 

@@ -1,13 +1,13 @@
 // y[p] = W x[row(p)] for 4-bit weights with a scale for every group of inputs (gs4 layers, layout in rmsmp.h), few tokens a matrix.
 //   y[p][m] = sum_u s[m][u] * (sum_{k in u} (code[m][k] - zero[m][u]) * x[k]),   u: runs of 32, 64 or 128 inputs
-// The inner sums are warp-level matrix instructions of 16 rows x 8 columns x 16 inputs: a code is turned into its exact fp16 or bf16 integer by
-// two or three logic operations and one subtraction for two codes, and no multiply-add is left for the CUDA cores but the one by the
-// scale, 4 for 16 x 8 x (32..128).  (One multiply-add and one conversion for each code would take 3 instructions a code; at the rate at which
-// memory delivers codes an SM has 2.7.)  Columns are tokens.  An fp32 token takes three: its bf16 parts, cut off 8 bits at a time, add up to it exactly.
-// A warp streams blocks of 16 rows x 128 inputs (1 KB of codes, one 16-byte load a lane and 64 inputs, all of a warp's next to each
-// other) kDepth blocks ahead in registers; a CTA's warps are `wr` row blocks x `wk` shares of the inputs, and a cluster of `split` CTAs shares the inputs
-// further where there are few rows.  Partial sums meet in shared memory, and across the cluster in distributed shared memory, in
-// a fixed order; no scratch memory, no atomics.
+// The inner sums are warp-level matrix instructions of 16 rows x 8 columns x 16 inputs on fp16 numbers with fp32 sums: a code becomes its exact
+// fp16 integer by five logic operations and four half2 additions for eight codes, and the CUDA cores have no multiply-add of their own but those
+// by the scale.  (fp16 whatever the activations' type: in bf16, whose last place is 1 at 128 where fp16's is 1 at 1024, every pair of codes
+// needs a shift of its own, 7 logic operations for eight; at half rate they are what bounds an SM.)  Columns are tokens; bf16 and fp32
+// activations come to fp16 by a power of two for every run and token, an fp32 one as two columns (see stage_x).
+// A warp streams blocks of 32 rows x 128 inputs (2 KB of codes) through a ring of its own in shared memory, filled by bulk copies; a CTA's warps are
+// `wr` row blocks x `wk` shares of the inputs, each CTA has `per` row blocks, and a cluster of `split` CTAs shares the inputs further where there are
+// few rows.  Partial sums meet in shared memory, and across the cluster in distributed shared memory, in a fixed order; no scratch memory, no atomics.
 #include <algorithm>
 #include "gs4.cuh"
 #include "ptx.cuh"
@@ -17,195 +17,221 @@ namespace rmsmp {
 namespace {
 
 constexpr int kWarps = 8, kThreads = kWarps * 32;
-constexpr int kDepth = 4;
-constexpr int kRed = 20;                 // floats between columns of a warp's 16-row partial sums (16, padded against bank conflicts)
+constexpr int kChunk = 2, kRing = 2;       // blocks of a copy; copies that a warp has in flight or at hand
+constexpr int kMostSmem = 226 * 1024;
+constexpr int kRed = 36;                 // floats between columns of a block's partial sums (32 rows, padded against bank conflicts)
 
 struct Plan {
     Gs4Args a;
     int wr, wk, split;                   // row blocks x input shares of a CTA's warps; CTAs of a cluster
+    int per, groups;                     // row blocks of a CTA (a multiple of wr); CTAs (clusters) that share a matrix's rows
     int slice, slab;                     // inputs of a CTA, and of one stage of x in shared memory (multiples of 128)
-    int groups;                          // groups of wr row blocks
-    int tokens;                          // tokens of one pass over the weights
-    int parts;                           // columns of a token
+    int tokens, parts;                   // tokens of one pass over the weights; columns of a token
 };
 
-template <bool kBf>
-__device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+// c = a * b + (kFirst ? 0 : c)
+template <bool kFirst>
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
-    if (kBf)
-        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    if (kFirst)
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+            : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
     else
         asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// What is subtracted from the codes of rows g and g + 8 (see expand).
-struct Zeros { uint32_t lo, hi; };
-template <bool kBf>
-__device__ __forceinline__ Zeros zeros_of(uint32_t byte)
+// (w & mask) | magic in one instruction; the mask is part of it
+template <uint32_t kMask>
+__device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t magic)
 {
-    const uint32_t zl = byte & 15u, zh = byte >> 4 & 15u;
-    if (kBf) return {(0x4300u + zl) * 0x10001u, (0x4300u + zh) * 0x10001u};          // 128 + z
-    return {(0x6400u + zl) * 0x10001u, (0xD400u + (zh << 4)) * 0x10001u};            // 1024 + z; -(64 + z)
+    uint32_t d;
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(w), "n"(kMask), "r"(magic));
+    return d;
+}
+__device__ __forceinline__ uint32_t constant(uint32_t v)                             // in a register, and kept there
+{
+    uint32_t r;
+    asm volatile("mov.u32 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
 }
 // Eight codes to four pairs code - zero, exactly.  A code in the low bits of the fp16 number 1024 adds itself to it, four bits further up
-// 16 times itself; in bf16, whose last place is 1 at 128, it has to be in the low bits.
-template <bool kBf>
-__device__ __forceinline__ void expand(uint32_t w, const Zeros& z, uint32_t (&r)[4])
-{
-    if (kBf) {
+// 16 times itself.
+struct Expander {
+    uint32_t magic = constant(0x64006400u), sixteenth = constant(0x2C002C00u);
+    uint32_t lo[2], hi[2];                                                           // 1024 + z and -(64 + z): rows g and g + 8 of each 16
+    __device__ __forceinline__ void set(uint32_t word)
+    {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint32_t v = ((w >> (4 * i)) & 0x000F000Fu) | 0x43004300u;
-            const uint32_t zz = i & 1 ? z.hi : z.lo;
-            __nv_bfloat162 d = __hsub2(reinterpret_cast<__nv_bfloat162&>(v), reinterpret_cast<const __nv_bfloat162&>(zz));
-            r[i] = reinterpret_cast<uint32_t&>(d);
+        for (int h = 0; h < 2; ++h) {
+            lo[h] = (0x6400u + (word >> (8 * h) & 15u)) * 0x10001u;
+            hi[h] = (0xD400u + (word >> (8 * h) & 0xF0u)) * 0x10001u;
         }
-    } else {
-        const uint32_t sixteenth = 0x2C002C00u;
+    }
+    __device__ __forceinline__ void operator()(uint32_t w, int h, uint32_t (&r)[4]) const
+    {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const uint32_t s = w >> (8 * i);
-            uint32_t lo = (s & 0x000F000Fu) | 0x64006400u, hi = (s & 0x00F000F0u) | 0x64006400u;
-            __half2 a = __hsub2(reinterpret_cast<__half2&>(lo), reinterpret_cast<const __half2&>(z.lo));
-            __half2 b = __hfma2(reinterpret_cast<__half2&>(hi), reinterpret_cast<const __half2&>(sixteenth), reinterpret_cast<const __half2&>(z.hi));
-            r[2 * i] = reinterpret_cast<uint32_t&>(a);
-            r[2 * i + 1] = reinterpret_cast<uint32_t&>(b);
+            asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r[2 * i]) : "r"(and_or<0x000F000Fu>(s, magic)), "r"(lo[h]));
+            asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r[2 * i + 1]) : "r"(and_or<0x00F000F0u>(s, magic)), "r"(sixteenth), "r"(hi[h]));
         }
     }
-}
-
-// 16 rows x 128 inputs as one lane holds them.
-template <int kSums>
-struct Unit {
-    uint4 q[2];
-    uint32_t s[kSums];
-    uint32_t z;              // a byte a sum
 };
-template <int kSums>
-__device__ __forceinline__ void load_unit(Unit<kSums>& u, const Gs4Args& a, int64_t block, int lane)
-{
-    const uint4* q = reinterpret_cast<const uint4*>(a.codes) + block * 64 + lane;
-    u.q[0] = __ldg(q);
-    u.q[1] = __ldg(q + 32);
-    const int64_t at = block * 8 + (lane >> 2);
-    if (kSums == 1) {
-        u.s[0] = __ldg(reinterpret_cast<const uint32_t*>(a.scales) + at);
-        if (a.zeros) u.z = __ldg(a.zeros + at);
-    } else if (kSums == 2) {
-        const uint2 v = __ldg(reinterpret_cast<const uint2*>(a.scales) + at);
-        u.s[0] = v.x; u.s[kSums - 1] = v.y;
-        if (a.zeros) u.z = __ldg(reinterpret_cast<const uint16_t*>(a.zeros) + at);
-    } else {
-        const uint4 v = __ldg(reinterpret_cast<const uint4*>(a.scales) + at);
-        u.s[0] = v.x; u.s[kSums / 4] = v.y; u.s[kSums / 2] = v.z; u.s[kSums - 1] = v.w;
-        if (a.zeros) u.z = __ldg(reinterpret_cast<const uint32_t*>(a.zeros) + at);
-    }
-}
 
-// `x`: this lane's place in the staged activations, at the unit's first input.
-template <bool kBf, int kNT, int kSums>
-__device__ __forceinline__ void use_unit(const Unit<kSums>& u, const Gs4Args& a, uint32_t x, uint32_t col_bytes, float (&tot)[kNT][4])
+// Adds a block, 32 rows x 128 inputs, to the sums.  `codes`, `scales`, `zeros`: this lane's; `x`: this lane's places in the staged activations, at the block's first input; `f`: its columns' factors.
+template <int kNT, int kSums, bool kZeros, bool kFactor>
+__device__ __forceinline__ void use_block(const uint8_t* codes, const uint8_t* scales, const uint8_t* zeros, Expander& expand, int scale_bf16, const uint8_t* const (&x)[kNT], const float* f, float (&tot)[2][kNT][4])
 {
-    float acc[kNT][4];
-    Zeros z = zeros_of<kBf>(0x88u);
+    uint4 q[2][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) q[h][i] = *reinterpret_cast<const uint4*>(codes + (2 * h + i) * 512);
+    float acc[2][kNT][4];
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
-        const int sum = b * kSums / 4;
-        if (b * kSums % 4 == 0) {
-#pragma unroll
-            for (int t = 0; t < kNT; ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[t][i] = 0.0f;
-            if (a.zeros) z = zeros_of<kBf>(u.z >> (8 * sum));
-        }
+        const int run = b * kSums / 4;
+        const bool first = b * kSums % 4 == 0, last = (b + 1) * kSums % 4 == 0;
+        if (kZeros && first) expand.set(*reinterpret_cast<const uint16_t*>(zeros + run * 2));
         uint32_t xb[kNT][4];
 #pragma unroll
-        for (int t = 0; t < kNT; ++t)
-            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(xb[t][0]), "=r"(xb[t][1]), "=r"(xb[t][2]), "=r"(xb[t][3])
-                         : "r"(x + t * 8 * col_bytes + b * 64));
-        const uint4& q = u.q[b >> 1];
-        const uint32_t w[2] = {b & 1 ? q.z : q.x, b & 1 ? q.w : q.y};
+        for (int t = 0; t < kNT; ++t) *reinterpret_cast<uint4*>(xb[t]) = *reinterpret_cast<const uint4*>(x[t] + b * 64);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            uint32_t r[4];
-            expand<kBf>(w[j], z, r);
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t w[2] = {b & 1 ? q[h][b >> 1].z : q[h][b >> 1].x, b & 1 ? q[h][b >> 1].w : q[h][b >> 1].y};
 #pragma unroll
-            for (int t = 0; t < kNT; ++t) mma16816<kBf>(acc[t], r[0], r[1], r[2], r[3], xb[t][2 * j], xb[t][2 * j + 1]);
+            for (int j = 0; j < 2; ++j) {
+                uint32_t r[4];
+                expand(w[j], h, r);
+#pragma unroll
+                for (int t = 0; t < kNT; ++t) {
+                    if (first && j == 0) mma16816<true>(acc[h][t], r, xb[t][0], xb[t][1]);
+                    else mma16816<false>(acc[h][t], r, xb[t][2 * j], xb[t][2 * j + 1]);
+                }
+            }
         }
-        if ((b + 1) * kSums % 4 == 0) {
-            const float s0 = scale_value(u.s[sum] & 0xffffu, a.scale_bf16), s1 = scale_value(u.s[sum] >> 16, a.scale_bf16);
+        if (last) {
+            const uint2 s4 = *reinterpret_cast<const uint2*>(scales + run * 8);
+            const uint32_t pair[2] = {s4.x, s4.y};
+            float s[2][2];
+            if (scale_bf16) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) { s[h][0] = __uint_as_float(pair[h] << 16); s[h][1] = __uint_as_float(pair[h] & 0xffff0000u); }
+            } else {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    s[h][0] = __half2float(__ushort_as_half((unsigned short)(pair[h] & 0xffffu)));
+                    s[h][1] = __half2float(__ushort_as_half((unsigned short)(pair[h] >> 16)));
+                }
+            }
 #pragma unroll
             for (int t = 0; t < kNT; ++t) {
-                tot[t][0] = __fmaf_rn(s0, acc[t][0], tot[t][0]);
-                tot[t][1] = __fmaf_rn(s0, acc[t][1], tot[t][1]);
-                tot[t][2] = __fmaf_rn(s1, acc[t][2], tot[t][2]);
-                tot[t][3] = __fmaf_rn(s1, acc[t][3], tot[t][3]);
+                float2 factor;
+                if (kFactor) factor = *reinterpret_cast<const float2*>(f + run * (8 * kNT) + 8 * t);
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float v = kFactor ? acc[h][t][i] * (i & 1 ? factor.y : factor.x) : acc[h][t][i];
+                        tot[h][t][i] = __fmaf_rn(s[h][i >> 1], v, tot[h][t][i]);
+                    }
             }
         }
     }
 }
 
-// The three bf16 numbers, eight significant bits each, that add up to an fp32 number.  Cut off, not rounded: no part overflows.
-__device__ __forceinline__ void split3(float v, uint32_t (&h)[3])
-{
-    const uint32_t b = __float_as_uint(v);
-    h[0] = b >> 16;
-    const float hi = __uint_as_float(b & 0xffff0000u);
-    const bool finite = (b & 0x7f800000u) != 0x7f800000u;
-    if (!finite && (b & 0x7fffffu)) h[0] |= 0x40u;               // (a NaN whose bits are all in the lower half)
-    const float r1 = finite ? v - hi : 0.0f;
-    h[1] = __float_as_uint(r1) >> 16;
-    const float r2 = r1 - __uint_as_float(__float_as_uint(r1) & 0xffff0000u);
-    h[2] = __float_as_uint(r2) >> 16;
-}
+// 2^e, e in -149..127
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float(e >= -126 ? (uint32_t)(e + 127) << 23 : 1u << (e + 149)); }
 
-// Inputs k0 .. k0 + slab of `n` rows of x, from row p0 on, into shared memory: a column of `col_bytes` for each part of each token.
-__device__ __forceinline__ void stage_x(const Plan& p, uint8_t* xs, uint32_t col_bytes, int64_t p0, int n, int k0, int slab)
+// Inputs k0 .. k0 + slab of `n` rows of x, from row p0 on, into shared memory, a column of `col_bytes` for each part of each token, and the factors
+// ([run][column]).  fp16 goes as it is.  The others are scaled by 2^-e, 2^e <= 2^-14 max|x| < 2^(e+1) over the finite numbers of the run, so that the
+// largest is in 2^14..2^15: a bf16 number's 8 bits are then exact down to 2^-32 of that, where fp16's last place has become fixed.  An fp32 number is the
+// sum of two fp16 ones, each rounded to nearest: 2^-24 of it is left out at most.
+template <int kSums, int kX>
+__device__ __forceinline__ void stage_x(const Plan& p, uint8_t* xs, float* factors, int columns, uint32_t col_bytes, int64_t p0, int n, int k0, int slab)
 {
+    constexpr int kParts = kX == RMSMP_F32 ? 2 : 1;
     const Gs4Args& a = p.a;
     const int vecs = slab >> 3;
-    for (int i = threadIdx.x; i < n * vecs; i += kThreads) {
-        const int t = i / vecs, v = i - t * vecs, k = k0 + v * 8;
+    const int lg = min(32 - __clz(vecs - 1), 31 - __clz(kThreads));             // 2^lg threads a token; 16 vectors a block, so 16 lanes go through this together
+    for (int t = threadIdx.x >> lg; t < n; t += kThreads >> lg) {
         int64_t row = p0 + t;
         if (a.rows) row = a.rows[row];
-        const int have = row < 0 || row >= a.x_rows ? 0 : min(8, a.K - k);     // may be negative
-        uint8_t* dst = xs + (uint32_t)t * p.parts * col_bytes + v * 16;
-        if (a.x_type != RMSMP_F32) {
-            const uint16_t* src = static_cast<const uint16_t*>(a.x) + row * a.ld_x + k;
-            uint32_t o[4] = {0, 0, 0, 0};
+        const bool there = row >= 0 && row < a.x_rows;
+        for (int v = threadIdx.x & ((1 << lg) - 1); v < vecs; v += 1 << lg) {
+            const int k = k0 + v * 8;
+            const int have = there ? min(8, a.K - k) : 0;                       // may be negative
+            const int64_t at = row * a.ld_x + k;
+            uint8_t* const dst = xs + (uint32_t)(t * kParts) * col_bytes + v * 16;
+            uint32_t w[4 * kParts];
+#pragma unroll
+            for (int j = 0; j < 4 * kParts; ++j) w[j] = 0;
             if (have == 8 && a.x_vec) {
-                *reinterpret_cast<uint4*>(o) = *reinterpret_cast<const uint4*>(src);
+#pragma unroll
+                for (int j = 0; j < kParts; ++j) *reinterpret_cast<uint4*>(w + 4 * j) = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(a.x) + at * (2 * kParts) + 16 * j);
+            } else if (kX == RMSMP_F32) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (j < have) w[j & (4 * kParts - 1)] = static_cast<const uint32_t*>(a.x)[at + j];
             } else {
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    if (j < have) o[j >> 1] |= (uint32_t)src[j] << (16 * (j & 1));
+                    if (j < have) w[j >> 1] |= (uint32_t)static_cast<const uint16_t*>(a.x)[at + j] << (16 * (j & 1));
             }
-            *reinterpret_cast<uint4*>(dst) = make_uint4(o[0], o[1], o[2], o[3]);
-        } else {
-            const float* src = static_cast<const float*>(a.x) + row * a.ld_x + k;
-            float f[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-            if (have == 8 && a.x_vec) {
-                *reinterpret_cast<float4*>(f) = *reinterpret_cast<const float4*>(src);
-                *reinterpret_cast<float4*>(f + 4) = *reinterpret_cast<const float4*>(src + 4);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (j < have) f[j] = src[j];
+            if (kX == RMSMP_F16) {
+                *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
+                continue;
             }
-            uint32_t o[3][4] = {};
+            float f[8];
+            float most = 0.0f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                uint32_t h[3];
-                split3(f[j], h);
-                for (int q = 0; q < 3; ++q) o[q][j >> 1] |= h[q] << (16 * (j & 1));
+                f[j] = __uint_as_float(kX == RMSMP_F32 ? w[j & (4 * kParts - 1)] : j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16);
+                most = fmaxf(most, fabsf(f[j]));                                // (NaN is passed over)
             }
-            for (int q = 0; q < 3; ++q) *reinterpret_cast<uint4*>(dst + q * col_bytes) = make_uint4(o[q][0], o[q][1], o[q][2], o[q][3]);
+            if (most == INFINITY) {
+                most = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(f[j]) < INFINITY ? fabsf(f[j]) : 0.0f);
+            }
+            constexpr int kLanes = 16 / kSums;                                  // of a run
+            const uint32_t bits = __reduce_max_sync(((1u << kLanes) - 1) << (threadIdx.x & 31 & ~(kLanes - 1)), __float_as_uint(most));
+            const int e = max((int)(bits >> 23), 1) - 127 - 14;
+            if (e >= -126) {
+                const float up = power_of_two(-e);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f[j] *= up;
+            } else {                                                            // (2^140 is no fp32 number)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f[j] = f[j] * power_of_two(126) * power_of_two(-e - 126);
+            }
+            __half2 hi[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) hi[j] = __floats2half2_rn(f[2 * j], f[2 * j + 1]);
+            *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(hi);
+            if (kParts == 2) {
+                __half2 lo[4];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f[j] = fabsf(f[j]) < 65504.0f ? f[j] - (j & 1 ? __high2float(hi[j >> 1]) : __low2float(hi[j >> 1])) : 0.0f;      // (infinities and NaN: nothing)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) lo[j] = __floats2half2_rn(f[2 * j], f[2 * j + 1]);
+                *reinterpret_cast<uint4*>(dst + col_bytes) = *reinterpret_cast<const uint4*>(lo);
+            }
+            if (v % kLanes == 0) {
+                float* const to = factors + v / kLanes * columns + t * kParts;
+                to[0] = power_of_two(e);
+                if (kParts == 2) to[kParts - 1] = to[0];
+            }
         }
     }
 }
 
+// `bytes` (a multiple of 16) from global memory; the barrier counts them.
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
 __device__ __forceinline__ void cluster_arrive_wait()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -219,18 +245,39 @@ __device__ __forceinline__ float ld_cluster(uint32_t addr, int rank)
     return v;
 }
 
-template <bool kBf, int kNT, int kSums>
-__global__ void __launch_bounds__(kThreads, 2) gs4_mma_kernel(const __grid_constant__ Plan p)
+template <int kNT, int kSums, bool kZeros, int kX>
+__global__ void __launch_bounds__(kThreads, kNT == 4 ? 2 : 3) gs4_mma_kernel(const __grid_constant__ Plan p)
 {
-    extern __shared__ __align__(16) uint8_t smem[];
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ __align__(8) uint64_t s_full[kWarps][kRing];
+    __shared__ int s_abort;
+    constexpr int kCols = 8 * kNT;
+    constexpr bool kFactor = kX != RMSMP_F16;
+    constexpr int kBlockBytes = kCodeBytes + 64 * kSums + (kZeros ? 16 * kSums : 0);
+    const Gs4Args& a = p.a;
+    const bool scale_bf16 = a.scale_bf16;
+    const int lane = threadIdx.x & 31, warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);      // (the same for the whole warp to the compiler too)
+    Expander expand;
+    expand.set(0x8888u);
+    const uint32_t full = smem_u32(s_full[warp]);
+    if (lane == 0) {
+        for (int i = 0; i < kRing; ++i) mbar_init(full + i * 8, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_proxy_async_smem();
+    }
+    if (threadIdx.x == 0) s_abort = 0;
+    __syncthreads();
+    volatile int* abort_flag = &s_abort;
+    bool alive = true;
     pdl_wait();
     pdl_trigger();
-    constexpr int kCols = 8 * kNT;
-    Gs4Args a = p.a;
-    a.codes = pdl_ordered(a.codes); a.scales = pdl_ordered(a.scales); a.zeros = pdl_ordered(a.zeros);
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    uint8_t* const ring = smem + warp * (kRing * kChunk * kBlockBytes);
+    uint8_t* const xs = smem + kWarps * (kRing * kChunk * kBlockBytes);
+    const uint8_t *const codes = ring + lane * 16, *const scales = ring + kCodeBytes + (lane >> 2) * (8 * kSums);
+    const uint8_t* const zeros = ring + kCodeBytes + 64 * kSums + (lane >> 2) * (2 * kSums);
     const uint32_t col_bytes = (uint32_t)p.slab * 2 + 64;                       // (columns 64 bytes apart modulo 128: a lane group's eight loads touch every bank once)
-    float* red = reinterpret_cast<float*>(smem + kCols * col_bytes);            // [warp][column][kRed]
+    float* const factors = reinterpret_cast<float*>(xs + min(kCols, p.tokens * p.parts) * col_bytes);      // [run][column]
+    float* const red = factors + (kFactor ? p.slab / 128 * kSums * kCols : 0);                             // [row block][share][column][kRed]
 
     const int rank = blockIdx.x % p.split;
     const int rg = blockIdx.x / p.split % p.groups;
@@ -246,91 +293,148 @@ __global__ void __launch_bounds__(kThreads, 2) gs4_mma_kernel(const __grid_const
         end = min(begin + p.tokens, a.R);
     }
     const int wr = warp % p.wr, wk = warp / p.wr;
-    const int tile = rg * p.wr + wr;
-    const int units_k = a.Kp >> 7;                                              // of a whole row
-    const int64_t block0 = (matrix * a.tiles + min(tile, a.tiles - 1)) * units_k;
+    const uint32_t units_k = (uint32_t)a.Kp >> 7;                               // blocks of a whole row
+    const uint8_t* const blocks = a.blocks + matrix * a.tiles * units_k * kBlockBytes;
+    const int tile0 = rg * p.per, tiles = min(p.per, a.tiles - tile0);          // this CTA's row blocks
+    const int mine = tiles > wr ? (tiles - wr + p.wr - 1) / p.wr : 0;           // this warp's
     const int slice0 = rank * p.slice, slice1 = min(a.Kp, slice0 + p.slice);
-    const uint32_t x_lane = smem_u32(smem) + (lane >> 2) * col_bytes + (lane & 3) * 16;
+    int slot = 0;                                                               // of the ring, and the phase that its barrier is in
+    uint32_t phase = 0;
 
     for (int64_t p0 = begin; p0 < end; p0 += p.tokens) {
-        const int n = (int)min((int64_t)p.tokens, end - p0);
-        float tot[kNT][4];
+        const int n = (int)min((int64_t)p.tokens, end - p0), cols = n * p.parts;
+        // columns behind the last read the last one's inputs (their sums are dropped)
+        const uint8_t* x_lane[kNT];
 #pragma unroll
-        for (int t = 0; t < kNT; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) tot[t][i] = 0.0f;
-        for (int s0 = slice0; s0 < slice1; s0 += p.slab) {
-            const int slab = min(p.slab, slice1 - s0);
-            const int count = tile < a.tiles ? (slab / 128 - wk + p.wk - 1) / p.wk : 0;         // this warp's units
-            const int64_t first = block0 + s0 / 128 + wk;
-            Unit<kSums> u[kDepth];
-#pragma unroll
-            for (int d = 0; d < kDepth; ++d) {
-                u[d].z = 0;
-                if (d < count) load_unit(u[d], a, first + (int64_t)d * p.wk, lane);
-            }
+        for (int t = 0; t < kNT; ++t) x_lane[t] = xs + min(8 * t + (lane >> 2), cols - 1) * col_bytes + (lane & 3) * 16;
+        for (int s0 = slice0; s0 < slice1 || s0 == slice0; s0 += p.slab) {
+            const int units = max(0, min(p.slab, slice1 - s0)) / 128;
+            const int u0 = units * wk / p.wk, run = units * (wk + 1) / p.wk - u0;               // this warp's of every row block
+            // the block to fetch next, how many of its row are left, and row blocks
+            uint32_t next = (uint32_t)(tile0 + wr) * units_k + s0 / 128 + u0;
+            const uint32_t jump = (uint32_t)p.wr * units_k - run;
+            int left_next = run, rows_next = run > 0 ? mine : 0;
+            auto fetch = [&](int to) {
+                const int blocks_n = min(left_next, kChunk);
+                if (lane == 0) {
+                    mbar_arrive_expect_tx(full + to * 8, blocks_n * kBlockBytes);
+                    bulk_load(smem_u32(ring + to * (kChunk * kBlockBytes)), blocks + (uint64_t)next * (uint32_t)kBlockBytes, blocks_n * kBlockBytes, full + to * 8);
+                }
+                next += blocks_n;
+                left_next -= blocks_n;
+                if (left_next == 0) { next += jump; left_next = run; --rows_next; }
+            };
+            for (int d = 0; d < kRing && rows_next > 0 && alive; ++d) fetch((slot + d) % kRing);
             __syncthreads();                                                    // the last stage, and the last tokens' sums, are read
-            stage_x(p, smem, col_bytes, p0, n, s0, slab);
+            stage_x<kSums, kX>(p, xs, factors, kCols, col_bytes, p0, n, s0, units * 128);
             __syncthreads();
-            for (int i = 0; i < count; i += kDepth) {
+            float* sums = red + (wr * p.wk + wk) * kCols * kRed + (lane & 3) * 2 * kRed + (lane >> 2);       // of the row block at hand
+            for (int r = run > 0 ? mine : 0; r > 0 && alive; --r) {
+                const uint8_t* x[kNT];
+                float tot[2][kNT][4];
 #pragma unroll
-                for (int d = 0; d < kDepth; ++d)
-                    if (i + d < count) {
-                        use_unit<kBf, kNT, kSums>(u[d], a, x_lane + (uint32_t)((i + d) * p.wk + wk) * 256, col_bytes, tot);
-                        if (i + d + kDepth < count) load_unit(u[d], a, first + (int64_t)(i + d + kDepth) * p.wk, lane);
+                for (int t = 0; t < kNT; ++t) {
+                    x[t] = x_lane[t] + u0 * 256;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) tot[0][t][i] = tot[1][t][i] = 0.0f;
+                }
+                const float* f = factors + u0 * (kSums * kCols) + (lane & 3) * 2;
+                for (int left = run; left > 0; left -= kChunk) {
+                    alive = mbar_wait_step(full + slot * 8, phase, abort_flag);
+                    if (!alive) break;
+                    const int at = slot * (kChunk * kBlockBytes);
+#pragma unroll
+                    for (int c = 0; c < kChunk; ++c) {
+                        if (c > 0 && c >= left) break;
+                        const int o = at + c * kBlockBytes;
+                        use_block<kNT, kSums, kZeros, kFactor>(codes + o, scales + o, zeros + o, expand, scale_bf16, x, f, tot);
+#pragma unroll
+                        for (int t = 0; t < kNT; ++t) x[t] += 256;
+                        f += kSums * kCols;
                     }
+                    __syncwarp();
+                    if (rows_next > 0) fetch(slot);
+                    if (++slot == kRing) { slot = 0; phase ^= 1; }
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int t = 0; t < kNT; ++t)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            float* to = sums + (8 * t + (i & 1)) * kRed + 8 * (i >> 1) + 16 * h;
+                            if (8 * t + (lane & 3) * 2 + (i & 1) < cols) *to = s0 == slice0 ? tot[h][t][i] : *to + tot[h][t][i];
+                        }
+                sums += p.wr * p.wk * kCols * kRed;
             }
+            if (run == 0 && s0 == slice0)                                       // no inputs for this warp: its share is zero
+                for (int r = 0; r < mine; ++r, sums += p.wr * p.wk * kCols * kRed)
+                    for (int i = 0; i < kCols; i += 8)
+                        for (int j = 0; j < 4; ++j) sums[i * kRed + 8 * j] = sums[(i + 1) * kRed + 8 * j] = 0.0f;
         }
-        float* mine = red + warp * kCols * kRed;
-#pragma unroll
-        for (int t = 0; t < kNT; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) mine[(8 * t + (lane & 3) * 2 + (i & 1)) * kRed + (lane >> 2) + 8 * (i >> 1)] = tot[t][i];
         __syncthreads();
+        // 2^lg threads a column of the CTA's rows
+        const int rows = tiles * 32, lg = min(32 - __clz(rows - 1), 31 - __clz(kThreads)), step = kThreads >> lg;
+        const int r0 = threadIdx.x & ((1 << lg) - 1), t0 = threadIdx.x >> lg;
+        const int tile_floats = p.wk * kCols * kRed;
         if (p.split > 1) {
             // the CTA's own sum, over its warps' shares, in place of the first share's
-            for (int i = threadIdx.x; i < p.wr * 16 * n * p.parts; i += kThreads) {
-                const int r = i & 15, tile_of = (i >> 4) % p.wr, col = (i >> 4) / p.wr;
-                float v = 0.0f;
-                for (int k = 0; k < p.wk; ++k) v += red[((k * p.wr + tile_of) * kCols + col) * kRed + r];
-                red[(tile_of * kCols + col) * kRed + r] = v;
-            }
+            for (int col = t0; col < cols; col += step)
+                for (int r = r0; r < rows; r += 1 << lg) {
+                    float* const of = &red[(r >> 5) * tile_floats + col * kRed + (r & 31)];
+                    float v = 0.0f;
+                    for (int k = 0; k < p.wk; ++k) v += of[k * kCols * kRed];
+                    *of = v;
+                }
             cluster_arrive_wait();
         }
         const int shares = p.split > 1 ? p.split : p.wk;
-        for (int i = threadIdx.x + rank * kThreads; i < p.wr * 16 * n; i += kThreads * p.split) {
-            const int r = i & 15, tile_of = (i >> 4) % p.wr, t = (i >> 4) / p.wr;
-            const int m = (rg * p.wr + tile_of) * 16 + r;
-            float v = 0.0f;
-            for (int q = 0; q < p.parts; ++q) {
-                const int col = t * p.parts + q;
-                for (int k = 0; k < shares; ++k)
-                    v += p.split > 1 ? ld_cluster(smem_u32(&red[(tile_of * kCols + col) * kRed + r]), k)
-                                     : red[((k * p.wr + tile_of) * kCols + col) * kRed + r];
+        for (int t = t0 * p.split + rank; t < n; t += step * p.split)
+            for (int r = r0; r < rows; r += 1 << lg) {
+                const int m = tile0 * 32 + r;
+                if (m >= a.M) break;
+                float v = 0.0f;
+                for (int q = 0; q < p.parts; ++q) {
+                    const float* from = &red[(r >> 5) * tile_floats + (t * p.parts + q) * kRed + (r & 31)];
+                    for (int k = 0; k < shares; ++k) v += p.split > 1 ? ld_cluster(smem_u32(from), k) : from[k * kCols * kRed];
+                }
+                store_as(a.y, (p0 + t) * a.ld_y + m, a.y_type, v);
             }
-            if (m < a.M) store_as(a.y, (p0 + t) * a.ld_y + m, a.y_type, v);
-        }
         if (p.split > 1) cluster_arrive_wait();                                 // the others have read this CTA's sums
+    }
+    if (!alive) {
+        // a wait ran out: copies that are still under way are given the same time once more
+        volatile int again = 0;
+        for (int i = 0; i < kRing; ++i) mbar_wait(full + (slot + i) % kRing * 8, slot + i < kRing ? phase : phase ^ 1, &again);
+        if (lane == 0) atomicMax(a.status, (uint32_t)RMSMP_ERR_TIMEOUT);
     }
 }
 
-template <bool kBf, int kNT, int kSums>
+template <int kNT, int kSums, bool kZeros, int kX>
 cudaError_t launch_one(const Plan& p, int64_t grid, size_t smem, cudaStream_t st)
 {
     static bool attr_set[kMaxDevices] = {};
-    if (!ensure_smem_attr(reinterpret_cast<const void*>(gs4_mma_kernel<kBf, kNT, kSums>), 227 * 1024, attr_set)) return cudaErrorInvalidValue;
-    if (p.split == 1) return launch_dependent(gs4_mma_kernel<kBf, kNT, kSums>, (unsigned)grid, kThreads, smem, st, p);
-    return launch_dependent_cluster(gs4_mma_kernel<kBf, kNT, kSums>, p.split, (unsigned)grid, kThreads, smem, st, p);
+    auto* const kernel = gs4_mma_kernel<kNT, kSums, kZeros, kX>;
+    if (!ensure_smem_attr(reinterpret_cast<const void*>(kernel), kMostSmem, attr_set)) return cudaErrorInvalidValue;
+    if (p.split == 1) return launch_dependent(kernel, (unsigned)grid, kThreads, smem, st, p);
+    return launch_dependent_cluster(kernel, p.split, (unsigned)grid, kThreads, smem, st, p);
 }
-template <bool kBf, int kNT>
+template <int kNT, int kSums, bool kZeros>
+cudaError_t launch_type(const Plan& p, int64_t grid, size_t smem, cudaStream_t st)
+{
+    return p.a.x_type == RMSMP_F16    ? launch_one<kNT, kSums, kZeros, RMSMP_F16>(p, grid, smem, st)
+           : p.a.x_type == RMSMP_BF16 ? launch_one<kNT, kSums, kZeros, RMSMP_BF16>(p, grid, smem, st)
+                                      : launch_one<kNT, kSums, kZeros, RMSMP_F32>(p, grid, smem, st);
+}
+template <int kNT, int kSums>
+cudaError_t launch_kind(const Plan& p, int64_t grid, size_t smem, cudaStream_t st)
+{
+    return p.a.has_zeros ? launch_type<kNT, kSums, true>(p, grid, smem, st) : launch_type<kNT, kSums, false>(p, grid, smem, st);
+}
+template <int kNT>
 cudaError_t launch_sums(const Plan& p, int64_t grid, size_t smem, cudaStream_t st)
 {
-    return p.a.sums == 1 ? launch_one<kBf, kNT, 1>(p, grid, smem, st) : p.a.sums == 2 ? launch_one<kBf, kNT, 2>(p, grid, smem, st) : launch_one<kBf, kNT, 4>(p, grid, smem, st);
-}
-template <bool kBf>
-cudaError_t launch_columns(const Plan& p, int nt, int64_t grid, size_t smem, cudaStream_t st)
-{
-    return nt == 1 ? launch_sums<kBf, 1>(p, grid, smem, st) : nt == 2 ? launch_sums<kBf, 2>(p, grid, smem, st) : launch_sums<kBf, 4>(p, grid, smem, st);
+    return p.a.sums == 1 ? launch_kind<kNT, 1>(p, grid, smem, st) : p.a.sums == 2 ? launch_kind<kNT, 2>(p, grid, smem, st) : launch_kind<kNT, 4>(p, grid, smem, st);
 }
 
 }  // namespace
@@ -339,24 +443,41 @@ cudaError_t launch_gs4_product(const Gs4Args& a, cudaStream_t st)
 {
     Plan p;
     p.a = a;
-    p.parts = a.x_type == RMSMP_F32 ? 3 : 1;
+    p.parts = a.x_type == RMSMP_F32 ? 2 : 1;
     const int64_t expect = a.offsets ? std::max<int64_t>(1, (a.R + a.E - 1) / a.E) : a.R;      // tokens of a matrix
     const int nt = expect * p.parts <= 8 ? 1 : expect * p.parts <= 16 ? 2 : 4;
     p.tokens = 8 * nt / p.parts;
-    const int64_t many = a.offsets ? a.E : (a.R + p.tokens - 1) / p.tokens;
-    p.wr = 1;
-    while (p.wr < kWarps && a.tiles * many / (p.wr * 2) >= 2 * sm_count()) p.wr *= 2;
-    p.wk = kWarps / p.wr;
-    p.groups = (a.tiles + p.wr - 1) / p.wr;
-    p.split = 1;
-    while (p.split < 8 && p.groups * many * p.split * 2 <= 2 * sm_count() && a.Kp / 128 >= p.wk * p.split * 2) p.split *= 2;
-    p.slice = (a.Kp / 128 + p.split - 1) / p.split * 128;
-    const int most = (96 * 1024 / (8 * nt) - 64) / 2 / 128 * 128;
-    p.slab = std::min(p.slice, most);
-    const size_t smem = (size_t)8 * nt * (p.slab * 2 + 64) + (size_t)kWarps * 8 * nt * kRed * sizeof(float);
+    if (!a.offsets) p.tokens = (int)std::min<int64_t>(p.tokens, a.R);
+    const int64_t many = a.offsets ? a.E : (a.R + p.tokens - 1) / p.tokens, busy = a.offsets ? std::min<int64_t>(a.E, a.R) : many;
+    const int cols = p.tokens * p.parts, units = a.Kp / 128, sms = a.sms;
+    const size_t ring = (size_t)kWarps * kRing * kChunk * a.block_bytes;
+    const size_t column = 2, factor = a.x_type == RMSMP_F16 ? 0 : (size_t)a.sums * 8 * nt * sizeof(float);      // bytes: of an input and column; of 128 inputs
+    // Which rows and inputs a warp, a CTA and a cluster take: the least of an estimate in microseconds.  An SM streams 44 KB a microsecond, a warp alone
+    // a block in 0.4; x comes in at 40 KB a microsecond; a cluster's join takes 0.7, a second wave of CTAs 1.5.  (8192 x 8192, one bf16 token: 13.1 us with whole
+    // rows a CTA, 12.7 with quarters; eight fp16: over 30 and 15.3; 1024 x 1024: 3.5 and 4.3; 1024 x 4096, eight: 9.3 and 5.8.)
+    size_t smem = 0;
+    float best = 1e30f;
+    for (int wr = 1; wr <= kWarps; wr *= 2)
+        for (int split = 1; split <= 8 && split <= units; split *= 2) {
+            const int64_t rounds = std::max<int64_t>(1, (a.tiles * busy * split + 2 * sms * wr - 1) / (2 * (int64_t)sms * wr));      // row blocks of a warp that make one wave
+            const int per = (int)std::min<int64_t>(rounds, 8) * wr, wk = kWarps / wr;
+            const int64_t ctas = (a.tiles + per - 1) / per * busy * split, on_sm = (ctas + sms - 1) / sms;
+            const int slice = (units + split - 1) / split, blocks = (slice + wk - 1) / wk * (per / wr);
+            const size_t red = (size_t)per * wk * 8 * nt * kRed * sizeof(float), whole = red + ring + cols * 64;
+            const size_t need = whole + slice * (128 * column * cols + factor);
+            const float t = std::max(on_sm * blocks * kWarps * (a.block_bytes / 44e3f), on_sm * blocks * 0.2f + blocks * 0.2f) + slice * 256e-3f * cols / 40 + (split > 1 ? 0.7f : 0.0f) +
+                            1.5f * ((ctas - 1) / (2 * sms)) + (need > (size_t)kMostSmem / 2 && on_sm > 1 ? 2.0f : 0.0f);
+            if (t >= best || whole + 128 * column * cols + factor > (size_t)kMostSmem) continue;
+            best = t;
+            p.wr = wr; p.wk = wk; p.split = split; p.per = per;
+            p.groups = (a.tiles + per - 1) / per;
+            p.slice = slice * 128;
+            p.slab = (int)std::min<int64_t>(p.slice, (int64_t)((kMostSmem - whole) / (128 * column * cols + factor)) * 128);
+            smem = whole + p.slab * column * cols + p.slab / 128 * factor;
+        }
     const int64_t grid = many * p.groups * p.split;
     if (grid > (1ll << 31) - 1) return cudaErrorInvalidValue;
-    return a.x_type == RMSMP_F16 ? launch_columns<false>(p, nt, grid, smem, st) : launch_columns<true>(p, nt, grid, smem, st);
+    return nt == 1 ? launch_sums<1>(p, grid, smem, st) : nt == 2 ? launch_sums<2>(p, grid, smem, st) : launch_sums<4>(p, grid, smem, st);
 }
 
 }  // namespace rmsmp

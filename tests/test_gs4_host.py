@@ -25,13 +25,11 @@ def test_layout_of_a_layer():
                                  (1, 5, 100, 256, R.GS4_ZERO), (4096, 1, 1, 1 << 20, R.GS4_SYM), (1, 1 << 20, 1 << 20, 32, R.GS4_ZERO)]:
         L = R.rmsmp_gs4_layer_init(E, M, K, group, mode, R.F16)
         assert (L.E, L.M, L.K, L.group, L.mode, L.scale_type) == (E, M, K, group, mode, R.F16)
-        assert L.Kp == (K + 127) // 128 * 128 and L.tiles == (M + 15) // 16
+        assert L.Kp == (K + 127) // 128 * 128 and L.tiles == (M + 31) // 32
         assert L.sums == {0: 1, 64: 2}.get(group % 128, 4) and group % (128 // L.sums) == 0
-        blocks = E * L.tiles * (L.Kp // 128)
-        assert L.off_codes == 256 and L.off_scales >= L.off_codes + blocks * 1024
-        assert L.off_zeros >= L.off_scales + blocks * 8 * L.sums * 4
-        assert L.packed_bytes >= L.off_zeros + (blocks * 8 * L.sums if mode == R.GS4_ZERO else 0)
-        assert all(o % 256 == 0 for o in (L.off_codes, L.off_scales, L.off_zeros, L.packed_bytes))
+        assert L.block_bytes % 16 == 0 and L.block_bytes == 2048 + 64 * L.sums + (16 * L.sums if mode == R.GS4_ZERO else 0)
+        assert L.off_blocks % 256 == 0 and L.off_blocks >= 256 and L.packed_bytes % 256 == 0
+        assert L.packed_bytes >= L.off_blocks + E * L.tiles * (L.Kp // 128) * L.block_bytes
 
 
 @pytest.mark.parametrize("bad, status", [
@@ -61,7 +59,7 @@ def test_packing_refuses():
     refused(R.ERR_BUFFER_TOO_SMALL, R.rmsmp_gs4_pack_codes, L, BUF, BUF, BUF, BUF, 0)
     refused(R.ERR_ALIGN, R.rmsmp_gs4_pack_codes, L, BUF, BUF + 1, BUF, BUF, n)
     refused(R.ERR_NULL, R.rmsmp_gs4_unpack, L, BUF, None)
-    for field, value in (("magic", 1), ("Kp", 256), ("tiles", 2), ("sums", 1), ("off_scales", 1 << 40), ("packed_bytes", 0), ("M", 17), ("mode", 5)):
+    for field, value in (("magic", 1), ("Kp", 256), ("tiles", 2), ("sums", 1), ("off_blocks", 1 << 40), ("block_bytes", 16), ("packed_bytes", 0), ("M", 33), ("mode", 5)):
         bad = R.rmsmp_gs4_layer.from_buffer_copy(L)
         setattr(bad, field, value)
         refused(R.ERR_BAD_LAYER, R.rmsmp_gs4_quantize_pack, bad, BUF, R.F32, BUF, 1 << 30)
