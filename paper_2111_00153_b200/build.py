@@ -13,7 +13,7 @@ LIB = os.path.join(_HERE, "librmsmp.so")
 MARSHAL_SOURCE = os.path.join(CSRC, "marshal.cpp")
 # named for the interpreter it was built for, so that another one does not load it
 MARSHAL = os.path.join(_HERE, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
-SOURCES = ("host_api.cu", "pack.cu", "simt.cu", "tensor.cu", "tensor2.cu", "split.cu", "peak.cu", "builtin_scratch.cu", "stream.cu", "assign.cu", "depthwise.cu", "gather.cu", "gs4_api.cu", "gs4_pack.cu", "gs4_product.cu", "expert.cu")
+SOURCES = ("host_api.cu", "pack.cu", "simt.cu", "tensor.cu", "tensor2.cu", "split.cu", "peak.cu", "builtin_scratch.cu", "stream.cu", "assign.cu", "depthwise.cu", "gather.cu", "gs4_api.cu", "gs4_pack.cu", "gs4_product.cu", "gs4_tensor.cu", "expert.cu")
 HEADERS = tuple(sorted(f for f in os.listdir(CSRC) if f.endswith((".cuh", ".h")))) + \
           (os.path.join("..", "..", "include", "rmsmp.h"),)
 

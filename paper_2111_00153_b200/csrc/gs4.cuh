@@ -26,6 +26,7 @@ cudaError_t launch_gs4_quantize(const rmsmp_gs4_layer& L, const void* dW, int w_
 cudaError_t launch_gs4_pack(const rmsmp_gs4_layer& L, const uint8_t* codes, const void* scale, const uint8_t* zero, uint8_t* blob, cudaStream_t st);
 cudaError_t launch_gs4_unpack(const rmsmp_gs4_layer& L, const uint8_t* blob, uint8_t* codes, void* scale, uint8_t* zero, cudaStream_t st);
 cudaError_t launch_gs4_product(const Gs4Args& a, cudaStream_t st);
+cudaError_t launch_gs4_tensor(const Gs4Args& a, cudaStream_t st);
 
 cudaError_t launch_expert_sort(const int32_t* ids, int64_t P, int k, int E, int32_t* offsets, int32_t* rows, int32_t* place, cudaStream_t st);
 cudaError_t launch_expert_gather(const void* x, int size, int64_t x_rows, int64_t H, int64_t ld_x, const int32_t* rows, int64_t R, void* xs,

@@ -26,6 +26,7 @@ struct Plan {
     int wr, wk, split;                   // row blocks x input shares of a CTA's warps; CTAs of a cluster
     int per, groups;                     // row blocks of a CTA (a multiple of wr); CTAs (clusters) that share a matrix's rows
     int slice, slab;                     // inputs of a CTA, and of one stage of x in shared memory (multiples of 128)
+    int alone;                           // a warp has all inputs of its row blocks (wk = split = 1, one stage): it stores its sums itself
     int tokens, parts;                   // tokens of one pass over the weights; columns of a token
 };
 
@@ -79,8 +80,8 @@ struct Expander {
     }
 };
 
-// Adds a block, 32 rows x 128 inputs, to the sums.  `codes`, `scales`, `zeros`: this lane's; `x`: this lane's places in the staged activations, at the block's first input; `f`: its columns' factors.
-template <int kNT, int kSums, bool kZeros, bool kFactor>
+// Adds a block, 32 rows x 128 inputs, to the sums of the first kUsed of kNT times eight columns.  `codes`, `scales`, `zeros`: this lane's; `x`: this lane's places in the staged activations, at the block's first input; `f`: its columns' factors.
+template <int kNT, int kUsed, int kSums, bool kZeros, bool kFactor>
 __device__ __forceinline__ void use_block(const uint8_t* codes, const uint8_t* scales, const uint8_t* zeros, Expander& expand, int scale_bf16, const uint8_t* const (&x)[kNT], const float* f, float (&tot)[2][kNT][4])
 {
     uint4 q[2][2];
@@ -88,15 +89,15 @@ __device__ __forceinline__ void use_block(const uint8_t* codes, const uint8_t* s
     for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int i = 0; i < 2; ++i) q[h][i] = *reinterpret_cast<const uint4*>(codes + (2 * h + i) * 512);
-    float acc[2][kNT][4];
+    float acc[2][kUsed][4];
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
         const int run = b * kSums / 4;
         const bool first = b * kSums % 4 == 0, last = (b + 1) * kSums % 4 == 0;
         if (kZeros && first) expand.set(*reinterpret_cast<const uint16_t*>(zeros + run * 2));
-        uint32_t xb[kNT][4];
+        uint32_t xb[kUsed][4];
 #pragma unroll
-        for (int t = 0; t < kNT; ++t) *reinterpret_cast<uint4*>(xb[t]) = *reinterpret_cast<const uint4*>(x[t] + b * 64);
+        for (int t = 0; t < kUsed; ++t) *reinterpret_cast<uint4*>(xb[t]) = *reinterpret_cast<const uint4*>(x[t] + b * 64);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const uint32_t w[2] = {b & 1 ? q[h][b >> 1].z : q[h][b >> 1].x, b & 1 ? q[h][b >> 1].w : q[h][b >> 1].y};
@@ -105,7 +106,7 @@ __device__ __forceinline__ void use_block(const uint8_t* codes, const uint8_t* s
                 uint32_t r[4];
                 expand(w[j], h, r);
 #pragma unroll
-                for (int t = 0; t < kNT; ++t) {
+                for (int t = 0; t < kUsed; ++t) {
                     if (first && j == 0) mma16816<true>(acc[h][t], r, xb[t][0], xb[t][1]);
                     else mma16816<false>(acc[h][t], r, xb[t][2 * j], xb[t][2 * j + 1]);
                 }
@@ -126,7 +127,7 @@ __device__ __forceinline__ void use_block(const uint8_t* codes, const uint8_t* s
                 }
             }
 #pragma unroll
-            for (int t = 0; t < kNT; ++t) {
+            for (int t = 0; t < kUsed; ++t) {
                 float2 factor;
                 if (kFactor) factor = *reinterpret_cast<const float2*>(f + run * (8 * kNT) + 8 * t);
 #pragma unroll
@@ -246,7 +247,7 @@ __device__ __forceinline__ float ld_cluster(uint32_t addr, int rank)
 }
 
 template <int kNT, int kSums, bool kZeros, int kX>
-__global__ void __launch_bounds__(kThreads, kNT == 4 ? 2 : 3) gs4_mma_kernel(const __grid_constant__ Plan p)
+__global__ void __launch_bounds__(kThreads, kNT == 2 ? 2 : 3) gs4_mma_kernel(const __grid_constant__ Plan p)
 {
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ __align__(8) uint64_t s_full[kWarps][kRing];
@@ -298,6 +299,7 @@ __global__ void __launch_bounds__(kThreads, kNT == 4 ? 2 : 3) gs4_mma_kernel(con
     const int tile0 = rg * p.per, tiles = min(p.per, a.tiles - tile0);          // this CTA's row blocks
     const int mine = tiles > wr ? (tiles - wr + p.wr - 1) / p.wr : 0;           // this warp's
     const int slice0 = rank * p.slice, slice1 = min(a.Kp, slice0 + p.slice);
+    const bool alone = p.alone;                                                 // a warp has all inputs of its row blocks, in one stage
     int slot = 0;                                                               // of the ring, and the phase that its barrier is in
     uint32_t phase = 0;
 
@@ -347,7 +349,8 @@ __global__ void __launch_bounds__(kThreads, kNT == 4 ? 2 : 3) gs4_mma_kernel(con
                     for (int c = 0; c < kChunk; ++c) {
                         if (c > 0 && c >= left) break;
                         const int o = at + c * kBlockBytes;
-                        use_block<kNT, kSums, kZeros, kFactor>(codes + o, scales + o, zeros + o, expand, scale_bf16, x, f, tot);
+                        if (kNT == 1 || cols <= 8) use_block<kNT, 1, kSums, kZeros, kFactor>(codes + o, scales + o, zeros + o, expand, scale_bf16, x, f, tot);
+                        else use_block<kNT, kNT, kSums, kZeros, kFactor>(codes + o, scales + o, zeros + o, expand, scale_bf16, x, f, tot);
 #pragma unroll
                         for (int t = 0; t < kNT; ++t) x[t] += 256;
                         f += kSums * kCols;
@@ -365,13 +368,26 @@ __global__ void __launch_bounds__(kThreads, kNT == 4 ? 2 : 3) gs4_mma_kernel(con
                             float* to = sums + (8 * t + (i & 1)) * kRed + 8 * (i >> 1) + 16 * h;
                             if (8 * t + (lane & 3) * 2 + (i & 1) < cols) *to = s0 == slice0 ? tot[h][t][i] : *to + tot[h][t][i];
                         }
-                sums += p.wr * p.wk * kCols * kRed;
+                if (alone) {
+                    // nobody else adds to these rows
+                    __syncwarp();
+                    const int m = (tile0 + wr + (mine - r) * p.wr) * 32 + lane;
+                    for (int t = 0; t < n; ++t) {
+                        const float* from = red + wr * kCols * kRed + t * p.parts * kRed + lane;
+                        const float v = p.parts == 2 ? from[0] + from[kRed] : from[0];
+                        if (m < a.M) store_as(a.y, (p0 + t) * a.ld_y + m, a.y_type, v);
+                    }
+                    __syncwarp();
+                } else {
+                    sums += p.wr * p.wk * kCols * kRed;
+                }
             }
             if (run == 0 && s0 == slice0)                                       // no inputs for this warp: its share is zero
                 for (int r = 0; r < mine; ++r, sums += p.wr * p.wk * kCols * kRed)
                     for (int i = 0; i < kCols; i += 8)
                         for (int j = 0; j < 4; ++j) sums[i * kRed + 8 * j] = sums[(i + 1) * kRed + 8 * j] = 0.0f;
         }
+        if (alone) continue;
         __syncthreads();
         // 2^lg threads a column of the CTA's rows
         const int rows = tiles * 32, lg = min(32 - __clz(rows - 1), 31 - __clz(kThreads)), step = kThreads >> lg;
@@ -445,7 +461,8 @@ cudaError_t launch_gs4_product(const Gs4Args& a, cudaStream_t st)
     p.a = a;
     p.parts = a.x_type == RMSMP_F32 ? 2 : 1;
     const int64_t expect = a.offsets ? std::max<int64_t>(1, (a.R + a.E - 1) / a.E) : a.R;      // tokens of a matrix
-    const int nt = expect * p.parts <= 8 ? 1 : expect * p.parts <= 16 ? 2 : 4;
+    // Experts have more tokens than the average here and there: room for sixteen columns (the second eight are left out where there are none).
+    const int nt = expect * p.parts <= (a.offsets ? 2 : 8) ? 1 : 2;
     p.tokens = 8 * nt / p.parts;
     if (!a.offsets) p.tokens = (int)std::min<int64_t>(p.tokens, a.R);
     const int64_t many = a.offsets ? a.E : (a.R + p.tokens - 1) / p.tokens, busy = a.offsets ? std::min<int64_t>(a.E, a.R) : many;
@@ -459,17 +476,22 @@ cudaError_t launch_gs4_product(const Gs4Args& a, cudaStream_t st)
     float best = 1e30f;
     for (int wr = 1; wr <= kWarps; wr *= 2)
         for (int split = 1; split <= 8 && split <= units; split *= 2) {
-            const int64_t rounds = std::max<int64_t>(1, (a.tiles * busy * split + 2 * sms * wr - 1) / (2 * (int64_t)sms * wr));      // row blocks of a warp that make one wave
-            const int per = (int)std::min<int64_t>(rounds, 8) * wr, wk = kWarps / wr;
-            const int64_t ctas = (a.tiles + per - 1) / per * busy * split, on_sm = (ctas + sms - 1) / sms;
-            const int slice = (units + split - 1) / split, blocks = (slice + wk - 1) / wk * (per / wr);
-            const size_t red = (size_t)per * wk * 8 * nt * kRed * sizeof(float), whole = red + ring + cols * 64;
-            const size_t need = whole + slice * (128 * column * cols + factor);
+            const int wk = kWarps / wr, slice = (units + split - 1) / split;
+            const size_t shared_by_all = ring + cols * 64, stage = slice * (128 * column * cols + factor), sums = (size_t)wr * wk * 8 * nt * kRed * sizeof(float);
+            const bool alone = wk == 1 && split == 1 && shared_by_all + sums + stage <= (size_t)kMostSmem;
+            // row blocks of a warp: as many as make one wave
+            int64_t rounds = std::max<int64_t>(1, (a.tiles * busy * split + 2 * sms * wr - 1) / (2 * (int64_t)sms * wr));
+            if (!alone) rounds = std::min<int64_t>(rounds, 8);
+            rounds = std::min<int64_t>(rounds, (a.tiles + wr - 1) / wr);
+            const int per = (int)rounds * wr;
+            const size_t whole = shared_by_all + (alone ? sums : sums * rounds), need = whole + stage;
+            const int64_t ctas = (a.tiles + per - 1) / per * busy * split, on_sm = (ctas + sms - 1) / sms, at_once = need <= (size_t)kMostSmem / 2 ? 2 : 1;
+            const int blocks = (slice + wk - 1) / wk * (int)rounds;
             const float t = std::max(on_sm * blocks * kWarps * (a.block_bytes / 44e3f), on_sm * blocks * 0.2f + blocks * 0.2f) + slice * 256e-3f * cols / 40 + (split > 1 ? 0.7f : 0.0f) +
-                            1.5f * ((ctas - 1) / (2 * sms)) + (need > (size_t)kMostSmem / 2 && on_sm > 1 ? 2.0f : 0.0f);
+                            1.5f * ((ctas - 1) / (at_once * sms));
             if (t >= best || whole + 128 * column * cols + factor > (size_t)kMostSmem) continue;
             best = t;
-            p.wr = wr; p.wk = wk; p.split = split; p.per = per;
+            p.wr = wr; p.wk = wk; p.split = split; p.per = per; p.alone = alone;
             p.groups = (a.tiles + per - 1) / per;
             p.slice = slice * 128;
             p.slab = (int)std::min<int64_t>(p.slice, (int64_t)((kMostSmem - whole) / (128 * column * cols + factor)) * 128);
@@ -477,7 +499,7 @@ cudaError_t launch_gs4_product(const Gs4Args& a, cudaStream_t st)
         }
     const int64_t grid = many * p.groups * p.split;
     if (grid > (1ll << 31) - 1) return cudaErrorInvalidValue;
-    return nt == 1 ? launch_sums<1>(p, grid, smem, st) : nt == 2 ? launch_sums<2>(p, grid, smem, st) : launch_sums<4>(p, grid, smem, st);
+    return nt == 1 ? launch_sums<1>(p, grid, smem, st) : launch_sums<2>(p, grid, smem, st);
 }
 
 }  // namespace rmsmp
