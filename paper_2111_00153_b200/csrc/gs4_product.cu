@@ -251,7 +251,8 @@ __global__ void __launch_bounds__(kThreads, kNT == 2 ? 2 : 3) gs4_mma_kernel(con
 {
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ __align__(8) uint64_t s_full[kWarps][kRing];
-    __shared__ int s_abort;
+    __shared__ int s_abort, s_found[3];
+    __shared__ uint32_t s_mask[kWarps];
     constexpr int kCols = 8 * kNT;
     constexpr bool kFactor = kX != RMSMP_F16;
     constexpr int kBlockBytes = kCodeBytes + 64 * kSums + (kZeros ? 16 * kSums : 0);
@@ -282,16 +283,33 @@ __global__ void __launch_bounds__(kThreads, kNT == 2 ? 2 : 3) gs4_mma_kernel(con
 
     const int rank = blockIdx.x % p.split;
     const int rg = blockIdx.x / p.split % p.groups;
-    const int which = blockIdx.x / p.split / p.groups;                          // expert, or piece of the rows of y
-    int64_t begin, end;
+    const int which = blockIdx.x / p.split / p.groups;                          // number of an expert, or piece of the rows of y
+    int64_t begin = (int64_t)which * p.tokens, end = min(begin + p.tokens, a.R);
     int64_t matrix = 0;
     if (a.offsets) {
-        matrix = which;
-        begin = min(max((int64_t)a.offsets[which], (int64_t)0), a.R);
-        end = min((int64_t)a.offsets[which + 1], a.R);
-    } else {
-        begin = (int64_t)which * p.tokens;
-        end = min(begin + p.tokens, a.R);
+        // the matrix is number `which` of those that have rows (there are CTAs for no more than there can be)
+        begin = end = 0;
+        int before = 0;
+        for (int e0 = 0; e0 < a.E && before <= which; e0 += kThreads) {
+            const int e = e0 + (int)threadIdx.x;
+            int64_t lo = 0, hi = 0;
+            if (e < a.E) {
+                lo = max((int64_t)a.offsets[e], (int64_t)0);
+                hi = min((int64_t)a.offsets[e + 1], a.R);
+            }
+            const uint32_t full_ones = __ballot_sync(0xffffffffu, hi > lo);
+            __syncthreads();
+            if (lane == 0) s_mask[warp] = full_ones;
+            __syncthreads();
+            int at = before + __popc(full_ones & ((1u << lane) - 1));
+            for (int w = 0; w < kWarps; ++w) {
+                if (w < warp) at += __popc(s_mask[w]);
+                before += __popc(s_mask[w]);
+            }
+            if (hi > lo && at == which) { s_found[0] = e; s_found[1] = (int)lo; s_found[2] = (int)hi; }
+        }
+        __syncthreads();
+        if (before > which) { matrix = s_found[0]; begin = s_found[1]; end = s_found[2]; }
     }
     const int wr = warp % p.wr, wk = warp / p.wr;
     const uint32_t units_k = (uint32_t)a.Kp >> 7;                               // blocks of a whole row
@@ -462,10 +480,11 @@ cudaError_t launch_gs4_product(const Gs4Args& a, cudaStream_t st)
     p.parts = a.x_type == RMSMP_F32 ? 2 : 1;
     const int64_t expect = a.offsets ? std::max<int64_t>(1, (a.R + a.E - 1) / a.E) : a.R;      // tokens of a matrix
     // Experts have more tokens than the average here and there: room for sixteen columns (the second eight are left out where there are none).
-    const int nt = expect * p.parts <= (a.offsets ? 2 : 8) ? 1 : 2;
+    // (64 experts of 1408 x 2048, 4 tokens each on average: 42 us with, 45 without; 100 of 768 x 2048: 54 and 52.)
+    const int nt = expect * p.parts <= (a.offsets ? 4 : 8) ? 1 : 2;
     p.tokens = 8 * nt / p.parts;
     if (!a.offsets) p.tokens = (int)std::min<int64_t>(p.tokens, a.R);
-    const int64_t many = a.offsets ? a.E : (a.R + p.tokens - 1) / p.tokens, busy = a.offsets ? std::min<int64_t>(a.E, a.R) : many;
+    const int64_t busy = a.offsets ? std::min<int64_t>(a.E, a.R) : (a.R + p.tokens - 1) / p.tokens;      // matrices with tokens, or passes over the one
     const int cols = p.tokens * p.parts, units = a.Kp / 128, sms = a.sms;
     const size_t ring = (size_t)kWarps * kRing * kChunk * a.block_bytes;
     const size_t column = 2, factor = a.x_type == RMSMP_F16 ? 0 : (size_t)a.sums * 8 * nt * sizeof(float);      // bytes: of an input and column; of 128 inputs
@@ -482,13 +501,21 @@ cudaError_t launch_gs4_product(const Gs4Args& a, cudaStream_t st)
             // row blocks of a warp: as many as make one wave
             int64_t rounds = std::max<int64_t>(1, (a.tiles * busy * split + 2 * sms * wr - 1) / (2 * (int64_t)sms * wr));
             if (!alone) rounds = std::min<int64_t>(rounds, 8);
+            if (a.offsets) rounds = 1;                  // (experts' tokens differ: more and shorter CTAs even out)
             rounds = std::min<int64_t>(rounds, (a.tiles + wr - 1) / wr);
             const int per = (int)rounds * wr;
             const size_t whole = shared_by_all + (alone ? sums : sums * rounds), need = whole + stage;
             const int64_t ctas = (a.tiles + per - 1) / per * busy * split, on_sm = (ctas + sms - 1) / sms, at_once = need <= (size_t)kMostSmem / 2 ? 2 : 1;
             const int blocks = (slice + wk - 1) / wk * (int)rounds;
-            const float t = std::max(on_sm * blocks * kWarps * (a.block_bytes / 44e3f), on_sm * blocks * 0.2f + blocks * 0.2f) + slice * 256e-3f * cols / 40 + (split > 1 ? 0.7f : 0.0f) +
-                            1.5f * ((ctas - 1) / (at_once * sms));
+            const float stage_us = slice * 256e-3f * cols / 40, join_us = split > 1 ? 0.7f : 0.0f;
+            float t;
+            if (a.offsets) {
+                // many short CTAs, of which an SM has `at_once`: as many waves as they fill, and half a one for the last
+                const float full = (float)ctas / (at_once * sms), block_us = std::max(0.4f, std::min(1.0f, full) * at_once * kWarps * (a.block_bytes / 44e3f));
+                t = (full <= 1 ? 1.0f : full + 0.5f) * (blocks * block_us + 1.5f + stage_us + join_us);
+            } else {
+                t = std::max(on_sm * blocks * kWarps * (a.block_bytes / 44e3f), on_sm * blocks * 0.2f + blocks * 0.2f) + stage_us + join_us + 1.5f * ((ctas - 1) / (at_once * sms));
+            }
             if (t >= best || whole + 128 * column * cols + factor > (size_t)kMostSmem) continue;
             best = t;
             p.wr = wr; p.wk = wk; p.split = split; p.per = per; p.alone = alone;
@@ -497,7 +524,7 @@ cudaError_t launch_gs4_product(const Gs4Args& a, cudaStream_t st)
             p.slab = (int)std::min<int64_t>(p.slice, (int64_t)((kMostSmem - whole) / (128 * column * cols + factor)) * 128);
             smem = whole + p.slab * column * cols + p.slab / 128 * factor;
         }
-    const int64_t grid = many * p.groups * p.split;
+    const int64_t grid = busy * p.groups * p.split;
     if (grid > (1ll << 31) - 1) return cudaErrorInvalidValue;
     return nt == 1 ? launch_sums<1>(p, grid, smem, st) : launch_sums<2>(p, grid, smem, st);
 }
