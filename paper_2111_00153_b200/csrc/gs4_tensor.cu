@@ -11,12 +11,14 @@
 #include <algorithm>
 #include "gs4.cuh"
 #include "ptx.cuh"
+#include "tmap.cuh"
 
 namespace rmsmp {
 
 namespace {
 
-constexpr int kWorkers = 512, kWorkWarps = kWorkers / 32, kThreads = kWorkers + 32;      // (the last warp issues)
+constexpr int kWorkers = 512, kWorkWarps = kWorkers / 32;
+constexpr int kIssuer = kWorkWarps, kCopier = kWorkWarps + 1;         // the warp that issues matrix instructions; the one that issues copies of x
 constexpr int kMostSmem = 226 * 1024;
 constexpr int kBytesA = 128 * 128 * 2;                    // operand A of 128 inputs: two tiles of 128 rows x 64 inputs
 constexpr int kOutPad = 4;                                // floats behind a token's 128 sums in shared memory
@@ -27,6 +29,7 @@ struct Plan {
     int split, units;                    // CTAs of a cluster; blocks of 128 inputs of each
     int mtiles, ntiles;                  // row tiles; token tiles (experts: as many as there can be)
     int y_vec;                           // four sums can be stored at once
+    CUtensorMap x_map;                   // of x: boxes of 64 inputs x kBN tokens (kBulk only)
 };
 
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar)
@@ -128,36 +131,51 @@ __device__ __forceinline__ void expand(uint32_t w, uint32_t lo, uint32_t hi, uin
     }
 }
 
+// (four deep as long as a stage has at most 32 KB)
 template <int kBN, int kX>
-constexpr int kStagesB = kBN * (kX == RMSMP_F32 ? 3 : 1) <= 64 ? 4 : 2;
+constexpr int kStagesB = kBN * (kX == RMSMP_F32 ? 3 : 1) <= 128 ? 4 : 2;
 template <int kBN, int kX>
 constexpr int kBytesB = kBN * 256 * (kX == RMSMP_F32 ? 3 : 1);      // operand B of 128 inputs: two tiles of kBN tokens x 64 inputs, three times in parts
 
-template <int kBN, int kX>
-__global__ void __launch_bounds__(kThreads, 1) gs4_tensor_kernel(const __grid_constant__ Plan p)
+template <bool kBulk> constexpr int kThreads = kWorkers + (kBulk ? 64 : 32);
+
+// kBulk: x comes by tensor copies (16-bit rows that start on 16 bytes and follow each other), else in the workers' hands.  (Gathered rows by tensor copies of
+// four rows: sixteen experts of 4096 x 1024 over 8192 rows 398 us, 174 by the workers.)
+template <int kBN, int kX, bool kBulk>
+__global__ void __launch_bounds__(kThreads<kBulk>, 1) gs4_tensor_kernel(const __grid_constant__ Plan p)
 {
+    constexpr bool kBf = kX != RMSMP_F16;
+    constexpr int kParts = kX == RMSMP_F32 ? 3 : 1, kSB = kStagesB<kBN, kX>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* const smem = smem_raw + (-smem_u32(smem_raw) & 1023u);
-    __shared__ __align__(8) uint64_t s_full[16], s_ready[2], s_done[2], s_free[2];
+    __shared__ __align__(8) uint64_t s_full[16], s_empty[16], s_ready[2], s_done[2], s_free[2], s_xfull[kSB], s_xempty[kSB];
     __shared__ uint64_t s_row[kBN];                                 // address of a token's inputs, 0: zeros
     __shared__ uint32_t s_tmem;
     __shared__ int s_abort, s_tile[3];
-    constexpr bool kBf = kX != RMSMP_F16;
-    constexpr int kParts = kX == RMSMP_F32 ? 3 : 1, kSB = kStagesB<kBN, kX>;
     constexpr int kCols = kBN / 4;                                  // tokens of a warp's sums
     constexpr int kLd = kCols < 16 ? kCols : 16;
     const Gs4Args& a = p.a;
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
     const int sums = a.sums;
     constexpr uint32_t kRunCols = kBN < 32 ? 32 : kBN, kTmemCols = 2 * kRunCols;      // two accumulators
-    if (warp == kWorkWarps) {
+    auto allocate = [&]() {
         // (in front of the trigger: a kernel that is placed early must not hold tensor memory that this one still has to get)
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "n"(kTmemCols) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-    }
+        if (warp == kIssuer) {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "n"(kTmemCols) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
+    };
+    if (!a.offsets) allocate();
     if (tid == 0) {
         s_abort = 0;
-        for (int i = 0; i < p.ring; ++i) mbar_init(smem_u32(&s_full[i]), 1);
+        for (int i = 0; i < p.ring; ++i) {
+            mbar_init(smem_u32(&s_full[i]), 1);
+            mbar_init(smem_u32(&s_empty[i]), kWorkWarps);
+        }
+        for (int i = 0; i < kSB; ++i) {
+            mbar_init(smem_u32(&s_xfull[i]), 1);
+            mbar_init(smem_u32(&s_xempty[i]), 1);
+        }
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&s_ready[i]), kWorkWarps);
             mbar_init(smem_u32(&s_done[i]), 1);
@@ -196,11 +214,13 @@ __global__ void __launch_bounds__(kThreads, 1) gs4_tensor_kernel(const __grid_co
             }
         }
         __syncthreads();
+        if (s_tile[0] < 0) return;                                  // (fewer tiles than there could be; the same for a whole cluster)
+        allocate();
     }
     const int expert = a.offsets ? s_tile[0] : 0;
     const int64_t p0 = a.offsets ? s_tile[1] : (int64_t)nt * kBN;
-    const int n = expert < 0 ? 0 : a.offsets ? s_tile[2] : (int)min((int64_t)kBN, a.R - p0);
-    for (int t = tid; t < kBN; t += kThreads) {
+    const int n = a.offsets ? s_tile[2] : (int)min((int64_t)kBN, a.R - p0);
+    for (int t = tid; t < kBN; t += kThreads<kBulk>) {
         uint64_t at = 0;
         if (t < n) {
             const int64_t row = a.rows ? a.rows[p0 + t] : p0 + t;
@@ -217,11 +237,11 @@ __global__ void __launch_bounds__(kThreads, 1) gs4_tensor_kernel(const __grid_co
     bool alive = true;
 
     const uint32_t units_k = (uint32_t)a.Kp >> 7;
-    const int unit0 = rank * p.units, units = n > 0 ? max(0, min(p.units, (int)units_k - unit0)) : 0;      // (an empty tile of experts goes straight to the end)
+    const int unit0 = rank * p.units, units = max(0, min(p.units, (int)units_k - unit0));
     uint8_t* const smem_a = smem;                                   // [2][kBytesA]
     uint8_t* const smem_b = smem + 2 * kBytesA;                     // [kSB][kBytesB]
     uint8_t* const ring = smem_b + kSB * kBytesB<kBN, kX>;          // [p.ring][4][block_bytes]
-    const uint8_t* const blocks = a.blocks + ((int64_t)max(expert, 0) * a.tiles + mt * 4) * units_k * a.block_bytes;
+    const uint8_t* const blocks = a.blocks + ((int64_t)expert * a.tiles + mt * 4) * units_k * a.block_bytes;
     const int row_blocks = min(4, a.tiles - mt * 4);
 
     const uint32_t slot_bytes = 4u * a.block_bytes;
@@ -231,24 +251,30 @@ __global__ void __launch_bounds__(kThreads, 1) gs4_tensor_kernel(const __grid_co
     for (int i = 0; i < kCols / 2; ++i) tot[i] = make_float2(0.0f, 0.0f);
     const int quarter = warp & 3, group = warp >> 2;                // a worker's rows (of the accumulators; its share of the codes' block `group`), and tokens
 
-    if (warp == kWorkWarps) {
+    if (warp == kIssuer) {
         // ---- the issuing warp: packed codes come in, matrix instructions go out
         int fetched = 0, fetch_slot = 0;
         const uint8_t* fetch_from = blocks + ((uint64_t)min(lane, row_blocks - 1) * units_k + unit0) * a.block_bytes;
+        uint32_t fetch_parity = 1;                                  // (the first round waits for nobody)
         auto fetch = [&]() {                                        // the next block
             const uint32_t bar = smem_u32(&s_full[fetch_slot]);
+            alive = mbar_wait_step(smem_u32(&s_empty[fetch_slot]), fetch_parity, abort_flag) && alive;
             if (lane == 0) mbar_arrive_expect_tx(bar, row_blocks * a.block_bytes);
             __syncwarp();
             if (lane < row_blocks) bulk_load(smem_u32(ring + fetch_slot * slot_bytes + lane * a.block_bytes), fetch_from, a.block_bytes, bar);
             fetch_from += a.block_bytes;
             ++fetched;
-            if (++fetch_slot == p.ring) fetch_slot = 0;
+            if (++fetch_slot == p.ring) { fetch_slot = 0; fetch_parity ^= 1; }
         };
         for (int u = 0; u < units && u < p.ring - 2; ++u) fetch();
         const uint32_t hi32 = (uint32_t)(smem_desc_kmajor(0, 128) >> 32), a0 = (smem_u32(smem_a) >> 4) | (1u << 16), b0 = (smem_u32(smem_b) >> 4) | (1u << 16);
-        uint32_t run = 0;
+        uint32_t run = 0, x_parity = 0;
         int stage = 0;
         for (int u = 0; u < units; ++u) {
+            // The block after next at the latest, into the slot of block u - 2, and in front of this block's instructions: with four runs the third waits
+            // until the first has been taken, which the workers do behind the operands of block u + 1.
+            if (fetched < units) fetch();
+            if (kBulk) alive = mbar_wait_step(smem_u32(&s_xfull[stage]), x_parity, abort_flag) && alive;
             alive = mbar_wait_step(smem_u32(&s_ready[u & 1]), (u >> 1) & 1, abort_flag) && alive;
             tc_fence_after();
             const uint32_t a_lo = a0 + (u & 1) * (kBytesA / 16), b_lo = b0 + stage * (kBytesB<kBN, kX> / 16);
@@ -272,8 +298,21 @@ __global__ void __launch_bounds__(kThreads, 1) gs4_tensor_kernel(const __grid_co
                 }
                 mma_commit_step(smem_u32(&s_done[run & 1]));
             }
-            if (++stage == kSB) stage = 0;
-            if (fetched < units) fetch();                           // (into the slot of block u - 2, whose accumulators have been taken, and so its scales)
+            if (kBulk) mma_commit_step(smem_u32(&s_xempty[stage]));
+            if (++stage == kSB) { stage = 0; x_parity ^= 1; }
+        }
+    } else if (kBulk && warp == kCopier) {
+        // ---- the copying warp: the tokens' inputs; K's end and rows that are not there read as zeros
+        int stage = 0;
+        uint32_t parity = 1;                                        // (the first round waits for nobody)
+        for (int u = 0; u < units; ++u) {
+            alive = mbar_wait_step(smem_u32(&s_xempty[stage]), parity, abort_flag) && alive;
+            const uint32_t bar = smem_u32(&s_xfull[stage]), to = smem_u32(smem_b) + stage * kBytesB<kBN, kX>;
+            const int k = (unit0 + u) * 128;
+            if (lane == 0) mbar_arrive_expect_tx(bar, kBN * 256);
+            __syncwarp();
+            if (lane < 2) tma_load_2d(to + lane * (kBN * 128), &p.x_map, bar, k + lane * 64, (int)p0);
+            if (++stage == kSB) { stage = 0; parity ^= 1; }
         }
     } else {
         // ---- the working warps
@@ -284,15 +323,21 @@ __global__ void __launch_bounds__(kThreads, 1) gs4_tensor_kernel(const __grid_co
         int stage_k = unit0 * 128;
         uint32_t stage_at = smem_u32(smem_b);
         const uint32_t stage_end = stage_at + kSB * kBytesB<kBN, kX>;
+        auto copy_x = [&](int j) {                                  // one token's part of the next block
+            const uint64_t at = s_row[min(xt + 32 * j, kBN - 1)];
+            if (kBN * 16 >= kWorkers || xt < kBN)
+                copy16(stage_at + x_dst + j * 4096, at != 0 ? at + (stage_k + xc * 8) * 2 : reinterpret_cast<uint64_t>(a.x), at != 0 ? 16u : 0u);
+        };
+        auto staged = [&]() {
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            stage_k += 128;
+            stage_at += kBytesB<kBN, kX>;
+            if (stage_at == stage_end) stage_at = smem_u32(smem_b);
+        };
         auto stage_x = [&]() {                                      // the tokens' inputs of the next block
             if (kX != RMSMP_F32 && a.x_vec && stage_k + 128 <= a.K) {
-                const uint32_t offset = (stage_k + xc * 8) * 2;
 #pragma unroll
-                for (int j = 0; j < kEach; ++j) {
-                    if (kBN * 16 < kWorkers && xt >= kBN) break;
-                    const uint64_t at = s_row[xt + 32 * j];
-                    copy16(stage_at + x_dst + j * 4096, at ? at + offset : reinterpret_cast<uint64_t>(a.x), at ? 16u : 0u);
-                }
+                for (int j = 0; j < kEach; ++j) copy_x(j);
             } else {
                 const int k = stage_k + xc * 8;
                 for (int j = 0; j < kEach; ++j) {
@@ -343,17 +388,16 @@ __global__ void __launch_bounds__(kThreads, 1) gs4_tensor_kernel(const __grid_co
                     for (int q = 0; q < 3; ++q) store16(dst + q * (kBN * 256), part[q]);
                 }
             }
-            asm volatile("cp.async.commit_group;" ::: "memory");
-            stage_k += 128;
-            stage_at += kBytesB<kBN, kX>;
-            if (stage_at == stage_end) stage_at = smem_u32(smem_b);
+            staged();
         };
 
         const uint8_t* const my_scales = ring + min(quarter, row_blocks - 1) * a.block_bytes + kCodeBytes + ((lane & 7) * sums * 4 + (lane >> 3)) * 2;
         const uint32_t my_tmem = tmem + ((uint32_t)quarter << 21) + group * kCols;
         const bool scale_bf16 = a.scale_bf16;
         uint32_t run = 0;
-        auto flush = [&](uint32_t slot_at) {                            // the accumulators of a block's runs, in turn
+        // The accumulators of a block's runs, in turn.  `with_x`: the copies of the next block's inputs, into what the last run's instructions have read, go out
+        // between the loads from tensor memory, whose latency they fill.
+        auto flush = [&](uint32_t slot_at, int slot, bool with_x) {
             for (int r = 0; r < sums; ++r, ++run) {
                 const float f = scale_value(*reinterpret_cast<const uint16_t*>(my_scales + slot_at + r * 8), scale_bf16);
                 const float2 s = make_float2(f, f);
@@ -366,11 +410,17 @@ __global__ void __launch_bounds__(kThreads, 1) gs4_tensor_kernel(const __grid_co
                     Columns<kLd>::load(at + c, v);
 #pragma unroll
                     for (int i = 0; i < kLd; i += 2) fma2(tot[(c + i) / 2], s, make_float2(v[i], v[i + 1]));
+                if (!kBulk && with_x && r == sums - 1) {
+                    constexpr int kSteps = kCols / kLd;
+#pragma unroll
+                    for (int j = c / kLd * kEach / kSteps; j < (c / kLd + 1) * kEach / kSteps; ++j) copy_x(j);
+                }
                 }
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&s_free[run & 1]));
             }
+            if (lane == 0) mbar_arrive(smem_u32(&s_empty[slot]));
         };
         // operand A: this warp's 16 rows x 64 inputs of block `group`
         const int half = quarter >> 1, part = quarter & 1, g = lane >> 2, odd = g & 1;      // (odd rows take their halves the other way round: rows 128 bytes apart would meet in the same banks)
@@ -381,11 +431,11 @@ __global__ void __launch_bounds__(kThreads, 1) gs4_tensor_kernel(const __grid_co
         const int zero0 = (2 * part + odd) * sums / 4 * 2, zero1 = (2 * part + 1 - odd) * sums / 4 * 2;
 
 #pragma unroll
-        for (int u = 0; u < kSB - 1; ++u) {
+        for (int u = 0; u < kSB - 1 && !kBulk; ++u) {
             if (u < units) stage_x();
             else asm volatile("cp.async.commit_group;" ::: "memory");
         }
-        int slot = 0;
+        int slot = 0, last_slot = 0;
         uint32_t slot_at = 0, last_at = 0, slot_parity = 0;
         for (int u = 0; u < units; ++u) {
             const uint32_t buf = u & 1;
@@ -412,19 +462,22 @@ __global__ void __launch_bounds__(kThreads, 1) gs4_tensor_kernel(const __grid_co
                     *reinterpret_cast<uint4*>(at + 8 * 128) = make_uint4(r0[1], r0[3], r1[1], r1[3]);
                 }
             }
-            asm volatile("cp.async.wait_group %0;" ::"n"(kSB - 2) : "memory");
+            if (!kBulk) asm volatile("cp.async.wait_group %0;" ::"n"(kSB - 2) : "memory");
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&s_ready[buf]));
-            if (u > 0) flush(last_at);
-            // (block u - 1's matrix instructions are over: its operands may go)
-            if (u + kSB - 1 < units) stage_x();
-            else asm volatile("cp.async.commit_group;" ::: "memory");
+            // (block u - 1's matrix instructions are over behind its last run: its operands may go)
+            const bool more = !kBulk && u + kSB - 1 < units, with_x = more && u > 0 && kX != RMSMP_F32 && a.x_vec && stage_k + 128 <= a.K;
+            if (u > 0) flush(last_at, last_slot, with_x);
+            if (with_x) staged();
+            else if (more) stage_x();
+            else if (!kBulk) asm volatile("cp.async.commit_group;" ::: "memory");
             last_at = slot_at;
+            last_slot = slot;
             slot_at += slot_bytes;
             if (++slot == p.ring) { slot = 0; slot_at = 0; slot_parity ^= 1; }
         }
-        if (units > 0) flush(last_at);
+        if (units > 0) flush(last_at, last_slot, false);
     }
 
     // sums to shared memory (operands and ring are done with), [token][128 rows]
@@ -435,7 +488,7 @@ __global__ void __launch_bounds__(kThreads, 1) gs4_tensor_kernel(const __grid_co
         if (warp < kWorkWarps) out[(group * kCols + i) * (128 + kOutPad) + quarter * 32 + lane] = i & 1 ? tot[i / 2].y : tot[i / 2].x;
     if (p.split > 1) cluster_arrive_wait(); else __syncthreads();
     const int m_left = a.M - mt * 128;
-    for (int i = tid + rank * kThreads; i < n * 32; i += kThreads * p.split) {
+    for (int i = tid + rank * kThreads<kBulk>; i < n * 32; i += kThreads<kBulk> * p.split) {
         const int t = i >> 5, m = (i & 31) * 4;
         float v[4];
         const float* from = out + t * (128 + kOutPad) + m;
@@ -481,39 +534,51 @@ __global__ void __launch_bounds__(kThreads, 1) gs4_tensor_kernel(const __grid_co
             }
             for (int u = max(0, units - p.ring); u < units && !again; ++u) mbar_wait(smem_u32(&s_full[u % p.ring]), (u / p.ring) & 1, &again);
         }
+        for (int i = 0; i < 200; ++i) __nanosleep(1000);            // (copies of x in flight land)
         if (lane == 0) atomicMax(a.status, (uint32_t)RMSMP_ERR_TIMEOUT);
     }
     __syncthreads();
-    if (warp == kWorkWarps) {
+    if (warp == kIssuer) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(kTmemCols) : "memory");
     }
 }
 
-template <int kBN, int kX>
+template <int kBN, int kX, bool kBulk>
 cudaError_t launch_one(Plan& p, cudaStream_t st)
 {
     static bool attr_set[kMaxDevices] = {};
-    auto* const kernel = gs4_tensor_kernel<kBN, kX>;
-    if (!ensure_smem_attr(reinterpret_cast<const void*>(kernel), kMostSmem - 8 * kBN, attr_set)) return cudaErrorInvalidValue;
-    const size_t fixed = 2 * kBytesA + (size_t)kStagesB<kBN, kX> * kBytesB<kBN, kX>, slot = 4 * (size_t)p.a.block_bytes;
-    p.ring = (int)std::min<size_t>(std::min<size_t>(16, (kMostSmem - 8 * kBN - 1024 - fixed) / slot), std::max(3, p.units + 2));
+    constexpr int kRoom = kMostSmem - 12 * kBN - 768;               // beside the static shared memory
+    auto* const kernel = gs4_tensor_kernel<kBN, kX, kBulk>;
+    if (!ensure_smem_attr(reinterpret_cast<const void*>(kernel), kRoom, attr_set)) return cudaErrorInvalidValue;
+    const size_t fixed = 1024 + 2 * kBytesA + (size_t)kStagesB<kBN, kX> * kBytesB<kBN, kX>, slot = 4 * (size_t)p.a.block_bytes;
+    p.ring = (int)std::min<size_t>(std::min<size_t>(16, (kRoom - fixed) / slot), std::max(3, p.units + 2));
     if (p.ring < 3) return cudaErrorInvalidValue;
-    const size_t smem = 1024 + std::max<size_t>(fixed + p.ring * slot, (size_t)kBN * (128 + kOutPad) * sizeof(float));
+    const size_t smem = std::max<size_t>(fixed + p.ring * slot, 1024 + (size_t)kBN * (128 + kOutPad) * sizeof(float));
     const int64_t grid = (int64_t)p.mtiles * p.ntiles * p.split;
     if (grid > (1ll << 31) - 1) return cudaErrorInvalidValue;
-    if (p.split == 1) return launch_dependent(kernel, (unsigned)grid, kThreads, smem, st, p);
-    return launch_dependent_cluster(kernel, p.split, (unsigned)grid, kThreads, smem, st, p);
+    if (kBulk) {
+        const cuuint64_t dim[2] = {(cuuint64_t)p.a.K, (cuuint64_t)p.a.x_rows}, pitch[1] = {(cuuint64_t)p.a.ld_x * 2};
+        const cuuint32_t box[2] = {64, (cuuint32_t)kBN}, step[2] = {1, 1};
+        if (tensor_map_encoder()(&p.x_map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, const_cast<void*>(p.a.x), dim, pitch, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                 CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+            return cudaErrorInvalidValue;
+    }
+    if (p.split == 1) return launch_dependent(kernel, (unsigned)grid, kThreads<kBulk>, smem, st, p);
+    return launch_dependent_cluster(kernel, p.split, (unsigned)grid, kThreads<kBulk>, smem, st, p);
 }
 template <int kX>
 cudaError_t launch_tokens(Plan& p, int bn, cudaStream_t st)
 {
+    constexpr bool kHalf = kX != RMSMP_F32;
+    // What the copy engine can address: 16-bit rows, one after the other, that start on 16 bytes.
+    const bool bulk = kHalf && !p.a.rows && p.a.x_vec && p.a.x_rows > 0 && (uint64_t)p.a.ld_x * 2 < (1ull << 40) && tensor_map_encoder();
     switch (bn) {
-        case 16: return launch_one<16, kX>(p, st);
-        case 32: return launch_one<32, kX>(p, st);
-        case 64: return launch_one<64, kX>(p, st);
-        case 128: return launch_one<kX == RMSMP_F32 ? 64 : 128, kX>(p, st);
-        default: return launch_one<kX == RMSMP_F32 ? 64 : 256, kX>(p, st);
+        case 16: return bulk ? launch_one<16, kX, kHalf>(p, st) : launch_one<16, kX, false>(p, st);
+        case 32: return bulk ? launch_one<32, kX, kHalf>(p, st) : launch_one<32, kX, false>(p, st);
+        case 64: return bulk ? launch_one<64, kX, kHalf>(p, st) : launch_one<64, kX, false>(p, st);
+        case 128: return bulk ? launch_one<kHalf ? 128 : 64, kX, kHalf>(p, st) : launch_one<kHalf ? 128 : 64, kX, false>(p, st);
+        default: return bulk ? launch_one<kHalf ? 256 : 64, kX, kHalf>(p, st) : launch_one<kHalf ? 256 : 64, kX, false>(p, st);
     }
 }
 
@@ -527,19 +592,22 @@ cudaError_t launch_gs4_tensor(const Gs4Args& a, cudaStream_t st)
     const int units = a.Kp / 128;
     const int64_t expect = a.offsets ? std::max<int64_t>(1, (a.R + a.E - 1) / a.E) : a.R;      // tokens of a matrix
     const int64_t busy = a.offsets ? std::min<int64_t>(a.E, a.R) : 1;
-    // Tokens of a tile and CTAs of a cluster: the least of an estimate.  A CTA takes `pace` microseconds for 128 inputs (measured: 4096 x 4096), 2.5 to start and
-    // to end, a cluster's join another; every SM has one CTA.
-    static constexpr struct { int bn; float pace; } kTiles[] = {{16, 0.75f}, {32, 0.78f}, {64, 0.83f}, {128, 1.05f}, {256, 1.9f}};
+    // Tokens of a tile and CTAs of a cluster: the least of an estimate.  A CTA takes `pace` microseconds for 128 inputs (measured: 4096 x 4096; `bulk`: x by tensor
+    // copies), 2.5 to start and to end, a cluster's join another; every SM has one CTA.
+    static constexpr struct { int bn; float pace, bulk; } kTiles[] = {{16, 0.75f, 0.72f}, {32, 0.78f, 0.75f}, {64, 0.83f, 0.8f}, {128, 1.05f, 0.95f}, {256, 1.7f, 1.25f}};
+    const bool bulk = !a.rows && a.x_vec;
     float best = 1e30f;
     int bn = 16;
     for (const auto& tile : kTiles) {
         if (tile.bn > 64 && a.x_type == RMSMP_F32) break;
-        const int64_t tiles = busy * ((expect + tile.bn - 1) / tile.bn) * p.mtiles;
+        // (experts' last tiles are half empty on average)
+        const float per = a.offsets ? std::max(1.0f, (float)expect / tile.bn + 0.5f) : (float)((expect + tile.bn - 1) / tile.bn);
+        const int64_t tiles = (int64_t)(busy * per * p.mtiles);
         for (int split = 1; split <= 4 && split <= units; split *= 2) {         // (clusters of eight wait for room: 1024 x 1024, 32 tokens 10.9 us, fours 5.5)
-            const float t = (float)((tiles * split + a.sms - 1) / a.sms) * ((units + split - 1) / split * tile.pace * (a.x_type == RMSMP_F32 ? 1.8f : 1.0f) + 2.5f + (split > 1 ? 1.0f : 0.0f));
+            const float t = (float)((tiles * split + a.sms - 1) / a.sms) * ((units + split - 1) / split * (bulk ? tile.bulk : tile.pace) * (a.x_type == RMSMP_F32 ? 1.8f : 1.0f) + 2.5f + (split > 1 ? 1.0f : 0.0f));
             if (t < best) { best = t; bn = tile.bn; p.split = split; }
         }
-        if (tile.bn >= expect) break;
+        if (tile.bn >= (a.offsets ? 4 : 1) * expect) break;
     }
     const int64_t ntiles = (a.R + bn - 1) / bn + (a.offsets ? std::min<int64_t>(a.E, a.R) : 0);
     if (ntiles > (1 << 30)) return cudaErrorInvalidValue;
