@@ -70,7 +70,7 @@ __global__ void __launch_bounds__(kSortThreads) expert_sort_kernel(const SortArg
         }
     };
     read(first);                                                 // (kept for the second walk where it is all)
-    for (int i = tid; i < a.warps * a.E; i += kSortThreads) count[i] = 0;
+    for (int i = tid; i < a.warps * a.E; i += (int)blockDim.x) count[i] = 0;
     __syncthreads();
     uint32_t* mine = count + warp * a.E;
     for (uint32_t i0 = first; i0 < last; i0 += 32 * kAhead) {
@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(kSortThreads) expert_sort_kernel(const SortArg
     if (lane == 31) s_warp[warp] = run;
     __syncthreads();
     uint32_t base = 0, pairs = 0;
-    for (int w = 0; w < kSortWarps; ++w) {
+    for (int w = 0; w < (int)blockDim.x / 32; ++w) {
         if (w < warp) base += s_warp[w];
         pairs += s_warp[w];
     }
@@ -144,7 +144,7 @@ __global__ void __launch_bounds__(kSortThreads) expert_sort_kernel(const SortArg
             if (kept) a.rows[at] = (int32_t)(i / a.k);
         }
     }
-    for (uint32_t p = pairs + (uint32_t)rank * kSortThreads + tid; p < a.P; p += (uint32_t)a.ctas * kSortThreads) a.rows[p] = -1;
+    for (uint32_t p = pairs + (uint32_t)rank * blockDim.x + tid; p < a.P; p += (uint32_t)a.ctas * blockDim.x) a.rows[p] = -1;
 }
 
 // ------------------------------------------------------------------ rows
@@ -395,8 +395,9 @@ cudaError_t sort_with(SortArgs a, cudaStream_t st)
     const uint32_t warps = (uint32_t)(a.ctas * a.warps);
     a.per_warp = std::max(1u, (a.P + warps * 32 - 1) / (warps * 32)) * 32;
     const size_t smem = sizeof(uint32_t) * (a.warps + 1) * (size_t)a.E;
+    const int threads = std::max(a.warps, (a.E + 31) / 32) * 32;           // a thread an expert, and the warps that have pairs
     if (!ensure_smem_attr(reinterpret_cast<const void*>(expert_sort_kernel), (kSortWarps + 1) * 1024 * 4, attr_set)) return cudaErrorInvalidValue;
-    if (a.ctas == 1) return launch_dependent(expert_sort_kernel, 1, kSortThreads, smem, st, a);
+    if (a.ctas == 1) return launch_dependent(expert_sort_kernel, 1, threads, smem, st, a);
     if (a.ctas > 8) {
         // (a cluster of sixteen is more than every device promises: where it cannot be had, eight)
         const int dev = device_ordinal();
@@ -405,7 +406,7 @@ cudaError_t sort_with(SortArgs a, cudaStream_t st)
             if (cudaFuncSetAttribute(expert_sort_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) cudaGetLastError();
         }
     }
-    const cudaError_t e = launch_dependent_cluster(expert_sort_kernel, a.ctas, a.ctas, kSortThreads, smem, st, a);
+    const cudaError_t e = launch_dependent_cluster(expert_sort_kernel, a.ctas, a.ctas, threads, smem, st, a);
     if (e == cudaSuccess || a.ctas <= 8) return e;
     a.ctas = 8;
     return sort_with(a, st);

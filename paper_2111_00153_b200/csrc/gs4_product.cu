@@ -156,30 +156,44 @@ __device__ __forceinline__ void stage_x(const Plan& p, uint8_t* xs, float* facto
     const Gs4Args& a = p.a;
     const int vecs = slab >> 3;
     const int lg = min(32 - __clz(vecs - 1), 31 - __clz(kThreads));             // 2^lg threads a token; 16 vectors a block, so 16 lanes go through this together
-    for (int t = threadIdx.x >> lg; t < n; t += kThreads >> lg) {
-        int64_t row = p0 + t;
-        if (a.rows) row = a.rows[row];
-        const bool there = row >= 0 && row < a.x_rows;
-        for (int v = threadIdx.x & ((1 << lg) - 1); v < vecs; v += 1 << lg) {
-            const int k = k0 + v * 8;
-            const int have = there ? min(8, a.K - k) : 0;                       // may be negative
-            const int64_t at = row * a.ld_x + k;
-            uint8_t* const dst = xs + (uint32_t)(t * kParts) * col_bytes + v * 16;
-            uint32_t w[4 * kParts];
+    const int v0 = threadIdx.x & ((1 << lg) - 1);
+    int t_next = v0 < vecs ? threadIdx.x >> lg : n, v_next = v0;
+    constexpr int kAhead = 1;                             // vectors that a thread has under way (one by one, eight tokens waited four times)
+    while (t_next < n) {
+        int ts[kAhead], vs[kAhead];
+        uint32_t ws[kAhead][4 * kParts];
 #pragma unroll
-            for (int j = 0; j < 4 * kParts; ++j) w[j] = 0;
+        for (int q = 0; q < kAhead; ++q) {
+            ts[q] = t_next; vs[q] = v_next;
+#pragma unroll
+            for (int j = 0; j < 4 * kParts; ++j) ws[q][j] = 0;
+            if (t_next >= n) continue;
+            int64_t row = p0 + t_next;
+            if (a.rows) row = a.rows[row];
+            const int k = k0 + v_next * 8;
+            const int have = row >= 0 && row < a.x_rows ? min(8, a.K - k) : 0;  // may be negative
+            const int64_t at = row * a.ld_x + k;
             if (have == 8 && a.x_vec) {
 #pragma unroll
-                for (int j = 0; j < kParts; ++j) *reinterpret_cast<uint4*>(w + 4 * j) = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(a.x) + at * (2 * kParts) + 16 * j);
+                for (int j = 0; j < kParts; ++j) *reinterpret_cast<uint4*>(ws[q] + 4 * j) = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(a.x) + at * (2 * kParts) + 16 * j);
             } else if (kX == RMSMP_F32) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    if (j < have) w[j & (4 * kParts - 1)] = static_cast<const uint32_t*>(a.x)[at + j];
+                    if (j < have) ws[q][j & (4 * kParts - 1)] = static_cast<const uint32_t*>(a.x)[at + j];
             } else {
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    if (j < have) w[j >> 1] |= (uint32_t)static_cast<const uint16_t*>(a.x)[at + j] << (16 * (j & 1));
+                    if (j < have) ws[q][j >> 1] |= (uint32_t)static_cast<const uint16_t*>(a.x)[at + j] << (16 * (j & 1));
             }
+            v_next += 1 << lg;
+            if (v_next >= vecs) { v_next = v0; t_next += kThreads >> lg; }
+        }
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) {
+            const int t = ts[q], v = vs[q];
+            if (t >= n) continue;
+            const uint32_t (&w)[4 * kParts] = ws[q];
+            uint8_t* const dst = xs + (uint32_t)(t * kParts) * col_bytes + v * 16;
             if (kX == RMSMP_F16) {
                 *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
                 continue;
@@ -271,8 +285,25 @@ __global__ void __launch_bounds__(kThreads, kNT == 2 ? 2 : 3) gs4_mma_kernel(con
     __syncthreads();
     volatile int* abort_flag = &s_abort;
     bool alive = true;
+    if (!a.offsets && p.split == 1 && lane == 0) {
+        // The first blocks on their way into the L2, which is where later writes go too: nothing is read ahead of the wait.  (4096 x 4096, one token: 6.0 us
+        // against 6.4; not for clusters, 4096 x 4096 for eight 10.2 against 9.2.)
+        const int tile = (int)(blockIdx.x % p.groups) * p.per + warp % p.wr, units = p.slab / 128, u0 = units * (warp / p.wr) / p.wk, run = units * (warp / p.wr + 1) / p.wk - u0;
+        if (run > 0 && tile < a.tiles)
+            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(a.blocks + ((uint64_t)tile * ((uint32_t)a.Kp >> 7) + u0) * kBlockBytes),
+                         "r"(min(run, kRing * kChunk) * kBlockBytes) : "memory");
+    }
     pdl_wait();
     pdl_trigger();
+    int block = blockIdx.x;
+    asm volatile("" : "+r"(block));                                             // (nothing of the above kept in registers)
+    const int rank = block % p.split;
+    const int rg = block / p.split % p.groups;
+    const int which = block / p.split / p.groups;                          // number of an expert, or piece of the rows of y
+    const int wr = warp % p.wr, wk = warp / p.wr;
+    const uint32_t units_k = (uint32_t)a.Kp >> 7;                               // blocks of a whole row
+    const int slice0 = rank * p.slice, slice1 = min(a.Kp, slice0 + p.slice);
+    const int tile0 = rg * p.per, tiles = min(p.per, a.tiles - tile0);          // this CTA's row blocks
     uint8_t* const ring = smem + warp * (kRing * kChunk * kBlockBytes);
     uint8_t* const xs = smem + kWarps * (kRing * kChunk * kBlockBytes);
     const uint8_t *const codes = ring + lane * 16, *const scales = ring + kCodeBytes + (lane >> 2) * (8 * kSums);
@@ -281,9 +312,6 @@ __global__ void __launch_bounds__(kThreads, kNT == 2 ? 2 : 3) gs4_mma_kernel(con
     float* const factors = reinterpret_cast<float*>(xs + min(kCols, p.tokens * p.parts) * col_bytes);      // [run][column]
     float* const red = factors + (kFactor ? p.slab / 128 * kSums * kCols : 0);                             // [row block][share][column][kRed]
 
-    const int rank = blockIdx.x % p.split;
-    const int rg = blockIdx.x / p.split % p.groups;
-    const int which = blockIdx.x / p.split / p.groups;                          // number of an expert, or piece of the rows of y
     int64_t begin = (int64_t)which * p.tokens, end = min(begin + p.tokens, a.R);
     int64_t matrix = 0;
     if (a.offsets) {
@@ -311,12 +339,8 @@ __global__ void __launch_bounds__(kThreads, kNT == 2 ? 2 : 3) gs4_mma_kernel(con
         __syncthreads();
         if (before > which) { matrix = s_found[0]; begin = s_found[1]; end = s_found[2]; }
     }
-    const int wr = warp % p.wr, wk = warp / p.wr;
-    const uint32_t units_k = (uint32_t)a.Kp >> 7;                               // blocks of a whole row
     const uint8_t* const blocks = a.blocks + matrix * a.tiles * units_k * kBlockBytes;
-    const int tile0 = rg * p.per, tiles = min(p.per, a.tiles - tile0);          // this CTA's row blocks
     const int mine = tiles > wr ? (tiles - wr + p.wr - 1) / p.wr : 0;           // this warp's
-    const int slice0 = rank * p.slice, slice1 = min(a.Kp, slice0 + p.slice);
     const bool alone = p.alone;                                                 // a warp has all inputs of its row blocks, in one stage
     int slot = 0;                                                               // of the ring, and the phase that its barrier is in
     uint32_t phase = 0;
