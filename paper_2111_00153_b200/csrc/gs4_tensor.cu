@@ -1,13 +1,18 @@
 // y[p] = W x[row(p)] for 4-bit weights with a scale for every group of inputs (gs4 layers, layout in rmsmp.h), on tcgen05: what the few-token
 // kernel (gs4_product.cu) would read the weights more than once or twice for.
 //   y[p][m] = sum_u s[m][u] * (sum_{k in u} (code[m][k] - zero[m][u]) * x[k]),   u: runs of 32, 64 or 128 inputs
-// A CTA takes 128 rows and kBN tokens.  For every 128 inputs its sixteen warps turn the packed codes into exact 16-bit floats of the activations'
-// type in shared memory (operand A, 128-byte swizzle), the tokens' inputs are copied beside them (operand B), and one thread issues the
-// matrix instructions, a run's into an accumulator of its own in tensor memory.  While they run, the warps take the accumulators of the 128 inputs
-// before, multiply each by its row's scale and add it to fp32 sums in registers.  Scales never touch the operands: a code times a scale would be rounded to 16 bits.
+// A CTA takes 128 rows and kBN tokens.  For every 128 inputs its sixteen working warps turn the packed codes into exact 16-bit floats of the activations'
+// type in shared memory (operand A, 128-byte swizzle), the tokens' inputs come beside them (operand B), and one warp issues the matrix instructions, a run's
+// into one of two accumulators in tensor memory.  While they run, the working warps take the accumulators of the 128 inputs before, multiply each
+// by its row's scale and add it to fp32 sums in registers.  Scales never touch the operands: a code times a scale, rounded to 16 bits, was tried (one accumulator
+// for all inputs, pairs of CTAs): 4096 x 4096 for 1024 bf16 tokens 52 us where this form took 65 then and takes 41 now, and 1.3 to 1.4 times the error.
 // An fp32 activation is three bf16 numbers (its bits cut 8 at a time: exact) that the same accumulator adds up, with three times the instructions.
-// A, B and the accumulators are double buffered (B four deep for few tokens), packed codes come through a ring of bulk copies.
+// Packed codes come through a ring of bulk copies.  x comes by tensor copies where its rows follow each other; in the workers' hands it costs as much time as all
+// the rest (64 KB a block for 256 tokens: 1378 cycles, codes to operand A 603, sums 850, of 3400).  Pairs of CTAs that share operand B (cta_group::2) halve that part
+// and lengthen the others, whose accesses meet the matrix instructions' in shared and tensor memory (sums 1570 cycles, the fence 600): 78 us for 65.
 // A cluster of `split` CTAs shares the inputs where there are few tiles; its sums meet in distributed shared memory, in a fixed order.
+// 4096 x 4096 for 1024 tokens: 41 us, 829 TFLOP/s, half of the measured 1679; 4096 x 1024 for 2048 in groups of 64: 29.8 us, 577.  What bounds it: the issue
+// slots, one multiply-add for two sums of every run beside the expansion, and the latency of loads from tensor memory while matrix instructions use it.
 #include <algorithm>
 #include "gs4.cuh"
 #include "ptx.cuh"
@@ -410,11 +415,11 @@ __global__ void __launch_bounds__(kThreads<kBulk>, 1) gs4_tensor_kernel(const __
                     Columns<kLd>::load(at + c, v);
 #pragma unroll
                     for (int i = 0; i < kLd; i += 2) fma2(tot[(c + i) / 2], s, make_float2(v[i], v[i + 1]));
-                if (!kBulk && with_x && r == sums - 1) {
-                    constexpr int kSteps = kCols / kLd;
+                    if (!kBulk && with_x && r == sums - 1) {
+                        constexpr int kSteps = kCols / kLd;
 #pragma unroll
-                    for (int j = c / kLd * kEach / kSteps; j < (c / kLd + 1) * kEach / kSteps; ++j) copy_x(j);
-                }
+                        for (int j = c / kLd * kEach / kSteps; j < (c / kLd + 1) * kEach / kSteps; ++j) copy_x(j);
+                    }
                 }
                 tc_fence_before();
                 __syncwarp();

@@ -175,6 +175,94 @@ def test_long_rows_and_many_rows(M, K, N, x_name):
     check_close(y, ref, absum, x_name, 48 + K / 128)
 
 
+@pytest.mark.parametrize("x_name", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("M, K, N, group, pad_x, pad_y", [(40, 70, 130, 32, 0, 0), (130, 1029, 300, 96, 0, 3), (520, 2304, 150, 64, 8, 4), (129, 640, 257, 128, 1, 0), (300, 130, 513, 64, 0, 2)])
+@pytest.mark.parametrize("mode", [R.GS4_SYM, R.GS4_ZERO])
+def test_many_tokens(M, K, N, group, pad_x, pad_y, mode, x_name):
+    p = Packed(M + N, 1, M, K, group, mode, "f16" if N & 1 else "bf16")
+    x = np.random.default_rng(N).standard_normal((N, K))
+    y, ref, absum = run_linear(p, x, x_name, x_name, pad_x, pad_y)
+    check_close(y, ref, absum, x_name, 48 + K / 128)
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("x_name", ["f16", "bf16"])
+def test_tiles_of_256_tokens(group, x_name):
+    """Enough tiles for every SM, the widest tiles, and more blocks of inputs than the ring of packed codes has slots."""
+    p = Packed(group, 1, 4096, 768, group, R.GS4_ZERO)
+    x = np.random.default_rng(group).standard_normal((1024, 768))
+    for pad in (0, 4):                                  # rows that the copy engine can address, and rows that it cannot
+        y, ref, absum = run_linear(p, x, x_name, x_name, pad, 0)
+        check_close(y, ref, absum, x_name, 54)
+
+
+@pytest.mark.parametrize("x_name", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("by_rows", [True, False])
+def test_experts_with_many_tokens(x_name, by_rows):
+    import torch
+    E, M, K, T, k = 5, 200, 400, 260, 2
+    p = Packed(E, E, M, K, 32, R.GS4_ZERO)
+    ids = route(3, T, k, E, 0.1)
+    ids[:, 0] = np.where(ids[:, 0] >= 0, 2, -1)         # one expert with far more than its share, which a token may name twice
+    offsets, rows, _ = G.sort_pairs(ids, E)
+    x = dev(np.random.default_rng(T).standard_normal((T, K)).astype(np.float32)).to(td(x_name))
+    xs = x if by_rows else x[dev(np.maximum(rows, 0)).long()].contiguous()
+    yb, y = framed(T * k, M, M + 1, x_name)
+    R.rmsmp_gs4_gemm_experts(p.layer, p.packed, xs, TYPES[x_name], xs.shape[0], K, dev(rows) if by_rows else None, dev(offsets), T * k, y, TYPES[x_name], M + 1)
+    torch.cuda.synchronize()
+    assert R.rmsmp_last_device_status(p.packed) == R.OK
+    out, hx = host(y), host(x)
+    for e in range(E):
+        a, b = offsets[e], offsets[e + 1]
+        if b > a:
+            ref, absum = G.product(p.w[e], hx[rows[a:b]])
+            check_close(out[a:b, :M], ref, absum, x_name, 52)
+    y[:offsets[-1], :M] = float("nan")
+    assert torch.isnan(yb).all()
+
+
+def test_rows_of_x_that_are_not_there():
+    """Fewer rows of x than of y, with and without an index: zeros."""
+    import torch
+    for Rn in (6, 100):
+        p = Packed(1, 2, 70, 96, 32, R.GS4_SYM)
+        for x_name in ("f32", "bf16"):
+            x = dev(np.random.default_rng(1).standard_normal((4, 96)).astype(np.float32)).to(td(x_name))
+            offsets = dev(np.array([0, Rn // 2, Rn], np.int32))
+            rows = np.arange(Rn, dtype=np.int32)
+            for index in (None, dev(rows)):
+                y = torch.full((Rn, 70), float("nan"), dtype=td(x_name), device="cuda")
+                R.rmsmp_gs4_gemm_experts(p.layer, p.packed, x, TYPES[x_name], 4, 96, index, offsets, Rn, y, TYPES[x_name], 70)
+                out = host(y)
+                for e in range(2):
+                    for q in range(e * (Rn // 2), Rn if e else Rn // 2):
+                        xr = host(x)[q:q + 1] if q < 4 else np.zeros((1, 96))
+                        ref, absum = G.product(p.w[e], xr)
+                        check_close(out[q:q + 1], ref, absum, x_name, 52)
+
+
+def test_two_streams_at_once():
+    """The same layer on two streams, many tokens on one and few on the other, again and again: nothing is shared but the weights."""
+    import torch
+    p = Packed(4, 1, 512, 1024, 64, R.GS4_ZERO)
+    rng = np.random.default_rng(4)
+    xs = [dev(rng.standard_normal((n, 1024)).astype(np.float32)).to(torch.bfloat16) for n in (3, 200)]
+    want = []
+    for x in xs:
+        y = torch.empty((x.shape[0], 512), dtype=torch.bfloat16, device="cuda")
+        R.rmsmp_gs4_gemm(p.layer, p.packed, x, R.BF16, x.shape[0], 1024, y, R.BF16, 512)
+        want.append(y)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    outs = [[torch.empty_like(w) for _ in range(20)] for w in want]
+    for i in range(20):
+        for s, x, o in zip(streams, xs, outs):
+            R.rmsmp_gs4_gemm(p.layer, p.packed, x, R.BF16, x.shape[0], 1024, o[i], R.BF16, 512, stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, w) for w, os in zip(want, outs) for o in os)
+    assert R.rmsmp_last_device_status(p.packed) == R.OK
+
+
 def test_no_tokens():
     import torch
     p = Packed(1, 1, 20, 40, 32, R.GS4_SYM)
