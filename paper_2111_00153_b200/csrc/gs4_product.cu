@@ -145,12 +145,12 @@ __device__ __forceinline__ void use_block(const uint8_t* codes, const uint8_t* s
 // 2^e, e in -149..127
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float(e >= -126 ? (uint32_t)(e + 127) << 23 : 1u << (e + 149)); }
 
-// Inputs k0 .. k0 + slab of `n` rows of x, from row p0 on, into shared memory, a column of `col_bytes` for each part of each token, and the factors
+// Inputs k0 .. k0 + slab of `n` rows of x (-1: zeros) into shared memory, a column of `col_bytes` for each part of each token, and the factors
 // ([run][column]).  fp16 goes as it is.  The others are scaled by 2^-e, 2^e <= 2^-14 max|x| < 2^(e+1) over the finite numbers of the run, so that the
 // largest is in 2^14..2^15: a bf16 number's 8 bits are then exact down to 2^-32 of that, where fp16's last place has become fixed.  An fp32 number is the
 // sum of two fp16 ones, each rounded to nearest: 2^-24 of it is left out at most.
 template <int kSums, int kX>
-__device__ __forceinline__ void stage_x(const Plan& p, uint8_t* xs, float* factors, int columns, uint32_t col_bytes, int64_t p0, int n, int k0, int slab)
+__device__ __forceinline__ void stage_x(const Plan& p, uint8_t* xs, float* factors, int columns, uint32_t col_bytes, const int* rows, int n, int k0, int slab)
 {
     constexpr int kParts = kX == RMSMP_F32 ? 2 : 1;
     const Gs4Args& a = p.a;
@@ -158,7 +158,7 @@ __device__ __forceinline__ void stage_x(const Plan& p, uint8_t* xs, float* facto
     const int lg = min(32 - __clz(vecs - 1), 31 - __clz(kThreads));             // 2^lg threads a token; 16 vectors a block, so 16 lanes go through this together
     const int v0 = threadIdx.x & ((1 << lg) - 1);
     int t_next = v0 < vecs ? threadIdx.x >> lg : n, v_next = v0;
-    constexpr int kAhead = 1;                             // vectors that a thread has under way (one by one, eight tokens waited four times)
+        constexpr int kAhead = 2;                             // vectors that a thread has under way (4096 x 4096, eight tokens: 9.1 us, one by one 9.5)
     while (t_next < n) {
         int ts[kAhead], vs[kAhead];
         uint32_t ws[kAhead][4 * kParts];
@@ -168,10 +168,8 @@ __device__ __forceinline__ void stage_x(const Plan& p, uint8_t* xs, float* facto
 #pragma unroll
             for (int j = 0; j < 4 * kParts; ++j) ws[q][j] = 0;
             if (t_next >= n) continue;
-            int64_t row = p0 + t_next;
-            if (a.rows) row = a.rows[row];
-            const int k = k0 + v_next * 8;
-            const int have = row >= 0 && row < a.x_rows ? min(8, a.K - k) : 0;  // may be negative
+            const int row = rows[t_next], k = k0 + v_next * 8;
+            const int have = row >= 0 ? min(8, a.K - k) : 0;                    // may be negative
             const int64_t at = row * a.ld_x + k;
             if (have == 8 && a.x_vec) {
 #pragma unroll
@@ -263,11 +261,11 @@ __device__ __forceinline__ float ld_cluster(uint32_t addr, int rank)
 template <int kNT, int kSums, bool kZeros, int kX>
 __global__ void __launch_bounds__(kThreads, kNT == 2 ? 2 : 3) gs4_mma_kernel(const __grid_constant__ Plan p)
 {
+    constexpr int kCols = 8 * kNT;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ __align__(8) uint64_t s_full[kWarps][kRing];
     __shared__ int s_abort, s_found[3];
-    __shared__ int s_passes[kWarps];
-    constexpr int kCols = 8 * kNT;
+    __shared__ int s_passes[kWarps], s_rows[kCols];
     constexpr bool kFactor = kX != RMSMP_F16;
     constexpr int kBlockBytes = kCodeBytes + 64 * kSums + (kZeros ? 16 * kSums : 0);
     const Gs4Args& a = p.a;
@@ -353,6 +351,10 @@ __global__ void __launch_bounds__(kThreads, kNT == 2 ? 2 : 3) gs4_mma_kernel(con
     uint32_t phase = 0;
 
     const int n = (int)(end - p0), cols = n * p.parts;
+    if ((int)threadIdx.x < n) {
+        const int64_t row = a.rows ? a.rows[p0 + threadIdx.x] : p0 + threadIdx.x;
+        s_rows[threadIdx.x] = row >= 0 && row < a.x_rows ? (int)row : -1;
+    }
     // columns behind the last read the last one's inputs (their sums are dropped)
     const uint8_t* x_lane[kNT];
 #pragma unroll
@@ -375,8 +377,8 @@ __global__ void __launch_bounds__(kThreads, kNT == 2 ? 2 : 3) gs4_mma_kernel(con
             if (left_next == 0) { next += jump; left_next = run; --rows_next; }
         };
         for (int d = 0; d < kRing && rows_next > 0 && alive; ++d) fetch((slot + d) % kRing);
-        __syncthreads();                                                    // the last stage is read
-        stage_x<kSums, kX>(p, xs, factors, kCols, col_bytes, p0, n, s0, units * 128);
+        __syncthreads();                                                    // the rows are there; the last stage is read
+        stage_x<kSums, kX>(p, xs, factors, kCols, col_bytes, s_rows, n, s0, units * 128);
         __syncthreads();
         float* sums = red + (wr * p.wk + wk) * kCols * kRed + (lane & 3) * 2 * kRed + (lane >> 2);       // of the row block at hand
         for (int r = run > 0 ? mine : 0; r > 0 && alive; --r) {
@@ -509,9 +511,8 @@ cudaError_t launch_gs4_product(const Gs4Args& a, cudaStream_t st)
     p.a = a;
     p.parts = a.x_type == RMSMP_F32 ? 2 : 1;
     const int64_t expect = a.offsets ? std::max<int64_t>(1, (a.R + a.E - 1) / a.E) : a.R;      // tokens of a matrix
-    // Experts have more tokens than the average here and there: room for sixteen columns (the second eight are left out where there are none).
-    // (64 experts of 1408 x 2048, 4 tokens each on average: 42 us with, 45 without; 100 of 768 x 2048: 54 and 52.)
-    const int nt = expect * p.parts <= (a.offsets ? 4 : 8) ? 1 : 2;
+    // (64 experts of 1408 x 2048, 4 tokens each on average: 35 us eight columns at a time, 40 sixteen; 8 tokens: 51 and 51; 16 tokens: 81 and 71.)
+    const int nt = expect * p.parts <= 8 ? 1 : 2;
     p.tokens = 8 * nt / p.parts;
     if (!a.offsets) p.tokens = (int)std::min<int64_t>(p.tokens, a.R);
     const int64_t busy = a.offsets ? std::min<int64_t>(a.E, a.R) : 1;                          // matrices with tokens, at most
@@ -537,14 +538,16 @@ cudaError_t launch_gs4_product(const Gs4Args& a, cudaStream_t st)
             const size_t whole = shared_by_all + (alone ? sums : sums * rounds), need = whole + stage;
             const int64_t ctas = (a.tiles + per - 1) / per * busy * split, on_sm = (ctas + sms - 1) / sms, at_once = need <= (size_t)kMostSmem / 2 ? 2 : 1;
             const int blocks = (slice + wk - 1) / wk * (int)rounds;
-            const float stage_us = slice * 256e-3f * cols / 40, join_us = split > 1 ? 0.7f : 0.0f;
             float t;
             if (a.offsets) {
-                // many short CTAs, of which an SM has `at_once`: as many waves as they fill, and half a one for the last
+                // Many short CTAs, of which an SM has `at_once`: as many waves as they fill, and half a one for the last.  4 us to start, find the tokens and end;
+                // x comes in at 10 KB a microsecond, behind the weights' first copies.  (64 experts of 1408 x 2048, 4 tokens each: eight row
+                // blocks a CTA 33 us, four 35, two 46; 8 tokens of 8: two 8.3, four 8.0, eight 11; eight experts of 4096 x 4096, 4 tokens: 24.3, halved in a cluster 23.4.)
                 const float full = (float)ctas / (at_once * sms), block_us = std::max(0.4f, std::min(1.0f, full) * at_once * kWarps * (a.block_bytes / 44e3f));
-                t = (full <= 1 ? 1.0f : full + 0.5f) * (blocks * block_us + 1.5f + stage_us + join_us);
+                t = (full <= 1 ? 1.0f : full + 0.5f) * (blocks * block_us + 4.0f + slice * 256e-4f * std::min<int64_t>(p.tokens, expect) * p.parts + (split > 1 ? 2.0f : 0.0f));
             } else {
-                t = std::max(on_sm * blocks * kWarps * (a.block_bytes / 44e3f), on_sm * blocks * 0.2f + blocks * 0.2f) + stage_us + join_us + 1.5f * ((ctas - 1) / (at_once * sms));
+                t = std::max(on_sm * blocks * kWarps * (a.block_bytes / 44e3f), on_sm * blocks * 0.2f + blocks * 0.2f) + slice * 256e-3f * cols / 40 +
+                    (split > 1 ? 0.7f : 0.0f) + 1.5f * ((ctas - 1) / (at_once * sms));
             }
             if (t >= best || whole + 128 * column * cols + factor > (size_t)kMostSmem) continue;
             best = t;

@@ -221,6 +221,31 @@ def test_experts_with_many_tokens(x_name, by_rows):
     assert torch.isnan(yb).all()
 
 
+@pytest.mark.parametrize("x_name", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("E, T, popular", [(6, 45, 2), (600, 300, 599), (600, 33, 256), (1, 7, 0)])
+def test_a_popular_expert_among_few_tokens(E, T, popular, x_name):
+    """Few tokens an expert on average, most of them with one: its tokens take several passes; more experts than a CTA has threads."""
+    import torch
+    M, K, k = 70, 300, 2
+    p = Packed(E + T, E, M, K, 32, R.GS4_SYM)
+    ids = route(T, T, k, E, 0.1)
+    ids[:, 0] = np.where(ids[:, 0] >= 0, popular, -1)
+    offsets, rows, _ = G.sort_pairs(ids, E)
+    x = dev(np.random.default_rng(T).standard_normal((T, K)).astype(np.float32)).to(td(x_name))
+    yb, y = framed(T * k, M, M + 2, x_name)
+    R.rmsmp_gs4_gemm_experts(p.layer, p.packed, x, TYPES[x_name], T, K, dev(rows), dev(offsets), T * k, y, TYPES[x_name], M + 2)
+    torch.cuda.synchronize()
+    assert R.rmsmp_last_device_status(p.packed) == R.OK
+    out, hx = host(y), host(x)
+    for e in range(E):
+        a, b = offsets[e], offsets[e + 1]
+        if b > a:
+            ref, absum = G.product(p.w[e], hx[rows[a:b]])
+            check_close(out[a:b, :M], ref, absum, x_name, 52)
+    y[:offsets[-1], :M] = float("nan")
+    assert torch.isnan(yb).all()
+
+
 def test_rows_of_x_that_are_not_there():
     """Fewer rows of x than of y, with and without an index: zeros."""
     import torch
