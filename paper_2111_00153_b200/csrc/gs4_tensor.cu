@@ -5,14 +5,16 @@
 // type in shared memory (operand A, 128-byte swizzle), the tokens' inputs come beside them (operand B), and one warp issues the matrix instructions, a run's
 // into one of two accumulators in tensor memory.  While they run, the working warps take the accumulators of the 128 inputs before, multiply each
 // by its row's scale and add it to fp32 sums in registers.  Scales never touch the operands: a code times a scale, rounded to 16 bits, was tried (one accumulator
-// for all inputs, pairs of CTAs): 4096 x 4096 for 1024 bf16 tokens 52 us where this form took 65 then and takes 41 now, and 1.3 to 1.4 times the error.
-// An fp32 activation is three bf16 numbers (its bits cut 8 at a time: exact) that the same accumulator adds up, with three times the instructions.
-// Packed codes come through a ring of bulk copies.  x comes by tensor copies where its rows follow each other; in the workers' hands it costs as much time as all
-// the rest (64 KB a block for 256 tokens: 1378 cycles, codes to operand A 603, sums 850, of 3400).  Pairs of CTAs that share operand B (cta_group::2) halve that part
-// and lengthen the others, whose accesses meet the matrix instructions' in shared and tensor memory (sums 1570 cycles, the fence 600): 78 us for 65.
+// for all inputs) and has 1.3 to 1.4 times the error.
+// An fp32 activation is three bf16 numbers (its bits cut 8 at a time: exact down to 2^-133) that the same accumulator adds up, with three times the instructions.
+// Packed codes come through a ring of bulk copies.  x comes by tensor copies where its rows follow each other, else in the workers' hands.
 // A cluster of `split` CTAs shares the inputs where there are few tiles; its sums meet in distributed shared memory, in a fixed order.
-// 4096 x 4096 for 1024 tokens: 41 us, 829 TFLOP/s, half of the measured 1679; 4096 x 1024 for 2048 in groups of 64: 29.8 us, 577.  What bounds it: the issue
-// slots, one multiply-add for two sums of every run beside the expansion, and the latency of loads from tensor memory while matrix instructions use it.
+// 4096 x 4096 for 1024 bf16 tokens: 42 us, 813 TFLOP/s, half of the measured 1679; 4096 x 1024 for 2048 in groups of 64: 31.9 us, 538.  What bounds it there is the
+// way of x from the L2: every 128 rows read it all, 268 MB in the first case.  Without expansion, instructions and sums the copies alone take 29 us of the 42;
+// without expansion and sums it is 40, without the instructions 37.  Tried against that: pairs of CTAs that share operand B (cta_group::2, 256 rows: half of the
+// reads, but every block waits for the other CTA: 63 us); operand A in tensor memory, which relieves shared memory (no room for two accumulators of 256 tokens;
+// 192: 39 us for 768 tokens, 41 this way); blocks of inputs in another order for every CTA (48 us: copies of the same x at the same time share their reads);
+// a warp of its own for the copies of codes, and their slots free before the sums are taken (46 us).  With few tokens it is the expansion, some 600 cycles a block.
 #include <algorithm>
 #include "gs4.cuh"
 #include "ptx.cuh"
@@ -162,7 +164,7 @@ __global__ void __launch_bounds__(kThreads<kBulk>, 1) gs4_tensor_kernel(const __
     const Gs4Args& a = p.a;
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
     const int sums = a.sums;
-    constexpr uint32_t kRunCols = kBN < 32 ? 32 : kBN, kTmemCols = 2 * kRunCols;      // two accumulators
+    constexpr uint32_t kRunCols = kBN < 32 ? 32 : kBN, kTmemCols = kBN == 192 ? 512 : 2 * kRunCols;      // two accumulators; a power of two
     auto allocate = [&]() {
         // (in front of the trigger: a kernel that is placed early must not hold tensor memory that this one still has to get)
         if (warp == kIssuer) {
@@ -583,6 +585,7 @@ cudaError_t launch_tokens(Plan& p, int bn, cudaStream_t st)
         case 32: return bulk ? launch_one<32, kX, kHalf>(p, st) : launch_one<32, kX, false>(p, st);
         case 64: return bulk ? launch_one<64, kX, kHalf>(p, st) : launch_one<64, kX, false>(p, st);
         case 128: return bulk ? launch_one<kHalf ? 128 : 64, kX, kHalf>(p, st) : launch_one<kHalf ? 128 : 64, kX, false>(p, st);
+        case 192: return bulk ? launch_one<kHalf ? 192 : 64, kX, kHalf>(p, st) : launch_one<kHalf ? 192 : 64, kX, false>(p, st);
         default: return bulk ? launch_one<kHalf ? 256 : 64, kX, kHalf>(p, st) : launch_one<kHalf ? 256 : 64, kX, false>(p, st);
     }
 }
@@ -599,7 +602,7 @@ cudaError_t launch_gs4_tensor(const Gs4Args& a, cudaStream_t st)
     const int64_t busy = a.offsets ? std::min<int64_t>(a.E, a.R) : 1;
     // Tokens of a tile and CTAs of a cluster: the least of an estimate.  A CTA takes `pace` microseconds for 128 inputs (measured: 4096 x 4096; `bulk`: x by tensor
     // copies), 2.5 to start and to end, a cluster's join another; every SM has one CTA.
-    static constexpr struct { int bn; float pace, bulk; } kTiles[] = {{16, 0.75f, 0.72f}, {32, 0.78f, 0.75f}, {64, 0.83f, 0.8f}, {128, 1.05f, 0.95f}, {256, 1.7f, 1.25f}};
+    static constexpr struct { int bn; float pace, bulk; } kTiles[] = {{16, 0.75f, 0.72f}, {32, 0.78f, 0.75f}, {64, 0.83f, 0.8f}, {128, 1.05f, 0.95f}, {192, 1.35f, 1.07f}, {256, 1.7f, 1.25f}};
     const bool bulk = !a.rows && a.x_vec;
     float best = 1e30f;
     int bn = 16;

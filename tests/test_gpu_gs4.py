@@ -196,6 +196,16 @@ def test_tiles_of_256_tokens(group, x_name):
         check_close(y, ref, absum, x_name, 54)
 
 
+@pytest.mark.parametrize("group", [32, 128])
+@pytest.mark.parametrize("N", [745, 768])
+@pytest.mark.parametrize("pad", [0, 4])
+def test_tiles_of_192_tokens(N, group, pad):
+    p = Packed(N + group, 1, 4096, 384, group, R.GS4_ZERO)
+    x = np.random.default_rng(N).standard_normal((N, 384))
+    y, ref, absum = run_linear(p, x, "bf16", "bf16", pad, 0)
+    check_close(y, ref, absum, "bf16", 51)
+
+
 @pytest.mark.parametrize("x_name", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("by_rows", [True, False])
 def test_experts_with_many_tokens(x_name, by_rows):
