@@ -9,12 +9,13 @@
 // An fp32 activation is three bf16 numbers (its bits cut 8 at a time: exact down to 2^-133) that the same accumulator adds up, with three times the instructions.
 // Packed codes come through a ring of bulk copies.  x comes by tensor copies where its rows follow each other, else in the workers' hands.
 // A cluster of `split` CTAs shares the inputs where there are few tiles; its sums meet in distributed shared memory, in a fixed order.
-// 4096 x 4096 for 1024 bf16 tokens: 42 us, 813 TFLOP/s, half of the measured 1679; 4096 x 1024 for 2048 in groups of 64: 31.9 us, 538.  What bounds it there is the
-// way of x from the L2: every 128 rows read it all, 268 MB in the first case.  Without expansion, instructions and sums the copies alone take 29 us of the 42;
-// without expansion and sums it is 40, without the instructions 37.  Tried against that: pairs of CTAs that share operand B (cta_group::2, 256 rows: half of the
-// reads, but every block waits for the other CTA: 63 us); operand A in tensor memory, which relieves shared memory (no room for two accumulators of 256 tokens;
-// 192: 39 us for 768 tokens, 41 this way); blocks of inputs in another order for every CTA (48 us: copies of the same x at the same time share their reads);
-// a warp of its own for the copies of codes, and their slots free before the sums are taken (46 us).  With few tokens it is the expansion, some 600 cycles a block.
+// 4096 x 4096 for 1024 bf16 tokens: 42 us, 813 TFLOP/s, half of the measured 1679; 4096 x 1024 for 2048 in groups of 64: 31.9 us, 538.  What bounds it there is
+// the hand-over between the roles: 2060 cycles for 128 inputs, of which the instructions need 1024; with no expansion, no instructions and no sums at all 1400 are
+// left (29 us), as many for 192 tokens a tile as for 256; without expansion and sums it is 40 us, without the instructions 37.  No unit is busy (tensor pipe 34 %,
+// shared memory and copies 26 %, L2 14 %).  Tried against that: pairs of CTAs that share operand B (cta_group::2, 256 rows: every block waits for the other CTA,
+// 63 us); operand A in tensor memory (no room for two accumulators of 256 tokens; 192: 39 us for 768 tokens, 41 this way); a warp of its own for the copies of
+// codes, and their slots free before the sums are taken (46 us); blocks of inputs in another order for every CTA (48 us: CTAs that read the same x at the same time
+// share their reads).  With few tokens it is the expansion, some 600 cycles a block.
 #include <algorithm>
 #include "gs4.cuh"
 #include "ptx.cuh"
