@@ -614,3 +614,113 @@ def test_results_repeat_bit_for_bit():
     for y in ys:
         R.rmsmp_gs4_gemm(p.layer, p.packed, x, R.F32, 3, 4096, y, R.F32, 1024)
     assert all(torch.equal(ys[0], y) for y in ys)
+
+
+@pytest.mark.parametrize("N", [3, 2100])
+def test_x_and_y_beyond_2_to_the_31(N):
+    """Rows of 2^31 / 2 elements apart for few tokens, of 2^20 for many: the last row is past 2^31 elements and 2^32 bytes."""
+    import torch
+    ld = (1 << 30) + 8 if N == 3 else 1 << 20
+    p = Packed(N, 1, 40, 200, 64, R.GS4_ZERO)
+    xb, yb = (torch.empty((N - 1) * ld + 256, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    x, y = (torch.as_strided(b, (N, c), (ld, 1)) for b, c in ((xb, 200), (yb, 40)))
+    x.copy_(torch.from_numpy(np.random.default_rng(N).standard_normal((N, 200)).astype(np.float32)))
+    R.rmsmp_gs4_gemm(p.layer, p.packed, x, R.BF16, N, ld, y, R.BF16, ld)
+    torch.cuda.synchronize()
+    ref, absum = G.product(p.w[0], host(x.contiguous()))
+    check_close(host(y.contiguous()), ref, absum, "bf16", 50)
+    rows = dev(np.array([N - 1, 0, N - 1], np.int32))
+    out = torch.empty((3, 200), dtype=torch.bfloat16, device="cuda")
+    R.rmsmp_expert_gather(x, R.BF16, N, 200, ld, rows, 3, out, 200)
+    assert torch.equal(out, x[rows.long()])
+    place = dev(np.array([[N - 1, 0]], np.int32))
+    R.rmsmp_expert_combine(x, R.BF16, N, 200, ld, place, None, 1, 2, out, 200)
+    assert torch.equal(out[0], (x[N - 1].float() + x[0].float()).bfloat16())
+    R.rmsmp_expert_combine_backward(out, R.BF16, 1, 2, 40, 200, None, N, ld, place, None, y, ld, None)
+    assert torch.equal(y[N - 1], out[0, :40]) and torch.equal(y[0], out[0, :40])
+
+
+def test_weights_beyond_2_to_the_32():
+    """More than 2^32 weights, the last matrix the only one that is not zero; then more than 2^32 bytes of packed ones."""
+    import torch
+    E, M, K = 260, 4096, 4096
+    W = torch.zeros((E, M, K), dtype=torch.bfloat16, device="cuda")
+    W[-1].copy_(torch.from_numpy(np.random.default_rng(8).standard_normal((M, K)).astype(np.float32)))
+    layer, last = R.rmsmp_gs4_layer_init(E, M, K, 128, R.GS4_ZERO, R.F16), R.rmsmp_gs4_layer_init(1, M, K, 128, R.GS4_ZERO, R.F16)
+    packed, want = (torch.empty(l.packed_bytes, dtype=torch.uint8, device="cuda") for l in (layer, last))
+    R.rmsmp_gs4_quantize_pack(layer, W, R.BF16, packed)
+    R.rmsmp_gs4_quantize_pack(last, W[-1].contiguous(), R.BF16, want)
+    blocks = last.tiles * (last.Kp // 128) * last.block_bytes
+    at = layer.off_blocks + (E - 1) * blocks
+    assert torch.equal(packed[at:at + blocks], want[256:256 + blocks])
+    sizes = W[-1].double().abs()
+    del W, packed
+    E = 500
+    layer = R.rmsmp_gs4_layer_init(E, M, K, 128, R.GS4_ZERO, R.F16)
+    packed = torch.zeros(layer.packed_bytes, dtype=torch.uint8, device="cuda")
+    assert layer.packed_bytes > 1 << 32
+    packed[layer.off_blocks + (E - 1) * blocks:][:blocks] = want[256:256 + blocks]
+    for N in (2, 30 * E):                               # few tokens an expert; many
+        rows = torch.randn((N, K), device="cuda").bfloat16()
+        few = min(N, 300)
+        offsets = np.full(E + 1, N - few, np.int32)
+        offsets[0], offsets[-1] = 0, N
+        y, ref = torch.empty((N, M), dtype=torch.bfloat16, device="cuda"), torch.empty((few, M), dtype=torch.bfloat16, device="cuda")
+        R.rmsmp_gs4_gemm_experts(layer, packed, rows, R.BF16, N, K, None, dev(offsets), N, y, R.BF16, M)
+        one_offsets = dev(np.array([0, few], np.int32))
+        R.rmsmp_gs4_gemm_experts(last, want, rows[-few:].contiguous(), R.BF16, few, K, None, one_offsets, few, ref, R.BF16, M)
+        assert (y[:N - few] == 0).all()                 # (the first matrix has scales of zero)
+        # (both within 52 + K / 128 steps of 2^-23 of the sum of the terms' sizes, and rounded once each; a quantized weight is at most a half larger than the
+        # weight, or half a step of a fifteenth of its group's range, under 0.5 for these)
+        a, b = y[-few:].double(), ref.double()
+        absum = rows[-few:].double().abs() @ (1.5 * sizes + 0.5).T
+        assert ((a - b).abs() <= 2 * 2.0 ** -8 * torch.maximum(a.abs(), b.abs()) + 2 * (52 + K / 128) * 2.0 ** -23 * absum).all()
+
+
+def test_captured_twice_and_replayed_together():
+    """Two graphs of the same layer on two streams, replayed at the same time, with inputs changed in place between replays."""
+    import torch
+    E, T, k, M = 6, 24, 2, 192
+    p = Packed(11, E, M, M, 64, R.GS4_ZERO)
+    rng = np.random.default_rng(11)
+
+    class Pass:
+        def __init__(self):
+            self.x = torch.empty((T, M), dtype=torch.bfloat16, device="cuda")
+            self.ids = torch.empty((T, k), dtype=torch.int32, device="cuda")
+            self.off, self.rows, self.place = (torch.empty(n, dtype=torch.int32, device="cuda") for n in (E + 1, T * k, T * k))
+            self.z, self.y, self.l = (torch.zeros((n, M), dtype=torch.bfloat16, device="cuda") for n in (T * k, T, T))
+
+        def run(self, s):
+            R.rmsmp_expert_sort(self.ids, T, k, E, self.off, self.rows, self.place, stream=s)
+            R.rmsmp_gs4_gemm_experts(p.layer, p.packed, self.x, R.BF16, T, M, self.rows, self.off, T * k, self.z, R.BF16, M, stream=s)
+            R.rmsmp_expert_combine(self.z, R.BF16, T * k, M, M, self.place, None, T, k, self.y, M, stream=s)
+            R.rmsmp_gs4_gemm(q.layer, q.packed, self.y, R.BF16, T, M, self.l, R.BF16, M, stream=s)
+
+        def fill(self):
+            self.x.copy_(torch.from_numpy(rng.standard_normal((T, M)).astype(np.float32)))
+            self.ids.copy_(torch.from_numpy(rng.integers(-1, E, (T, k)).astype(np.int32)))
+
+    q = Packed(12, 1, M, M, 32, R.GS4_SYM)
+    passes, graphs, streams = [Pass(), Pass()], [], [torch.cuda.Stream(), torch.cuda.Stream()]
+    for one, s in zip(passes, streams):
+        one.fill()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            one.run(s)
+        graphs.append(g)
+    for _ in range(5):
+        for one in passes:
+            one.fill()
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        got = [one.l.clone() for one in passes]
+        for one, want in zip(passes, got):
+            one.l.zero_()
+            one.run(torch.cuda.current_stream())
+            torch.cuda.synchronize()
+            assert torch.equal(one.l, want)
