@@ -17,7 +17,10 @@ namespace rmsmp {
 namespace {
 
 constexpr int kWarps = 8, kThreads = kWarps * 32;
-constexpr int kChunk = 2, kRing = 2;       // blocks of a copy; copies that a warp has in flight or at hand
+constexpr int kRing = 2;                 // copies that a warp has in flight or at hand
+// Blocks of a copy.  With sixteen columns, which many short CTAs of experts have, two CTAs fit on an SM if it is one (64 experts of 1408 x 2048, 16 tokens each:
+// 56 us, 70 with two; eight of 4096 x 4096, where one fits at most: 69 and 65); with eight they fit, and more in flight is better (2 tokens each: 21 us, 26 with one).
+__host__ __device__ constexpr int chunk_of(int nt) { return nt == 1 ? 2 : 1; }
 constexpr int kMostSmem = 226 * 1024;
 constexpr int kRed = 36;                 // floats between columns of a block's partial sums (32 rows, padded against bank conflicts)
 
@@ -27,6 +30,7 @@ struct Plan {
     int per, groups;                     // row blocks of a CTA (a multiple of wr); CTAs (clusters) that share a matrix's rows
     int slice, slab;                     // inputs of a CTA, and of one stage of x in shared memory (multiples of 128)
     int alone;                           // a warp has all inputs of its row blocks (wk = split = 1, one stage): it stores its sums itself
+    int single;                          // ... of its one row block, sixteen columns: they pass through its ring, which nothing comes into any more
     int tokens, parts;                   // tokens of one pass over the weights; columns of a token
 };
 
@@ -261,7 +265,7 @@ __device__ __forceinline__ float ld_cluster(uint32_t addr, int rank)
 template <int kNT, int kSums, bool kZeros, int kX>
 __global__ void __launch_bounds__(kThreads, kNT == 2 ? 2 : 3) gs4_mma_kernel(const __grid_constant__ Plan p)
 {
-    constexpr int kCols = 8 * kNT;
+    constexpr int kCols = 8 * kNT, kChunk = chunk_of(kNT);
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ __align__(8) uint64_t s_full[kWarps][kRing];
     __shared__ int s_abort, s_found[3];
@@ -380,7 +384,8 @@ __global__ void __launch_bounds__(kThreads, kNT == 2 ? 2 : 3) gs4_mma_kernel(con
         __syncthreads();                                                    // the rows are there; the last stage is read
         stage_x<kSums, kX>(p, xs, factors, kCols, col_bytes, s_rows, n, s0, units * 128);
         __syncthreads();
-        float* sums = red + (wr * p.wk + wk) * kCols * kRed + (lane & 3) * 2 * kRed + (lane >> 2);       // of the row block at hand
+        float* const first = kNT == 2 && p.single ? reinterpret_cast<float*>(ring) : red + (wr * p.wk + wk) * kCols * kRed;
+        float* sums = first + (lane & 3) * 2 * kRed + (lane >> 2);       // of the row block at hand
         for (int r = run > 0 ? mine : 0; r > 0 && alive; --r) {
             const uint8_t* x[kNT];
             float tot[2][kNT][4];
@@ -423,7 +428,7 @@ __global__ void __launch_bounds__(kThreads, kNT == 2 ? 2 : 3) gs4_mma_kernel(con
                 __syncwarp();
                 const int m = (tile0 + wr + (mine - r) * p.wr) * 32 + lane;
                 for (int t = 0; t < n; ++t) {
-                    const float* from = red + wr * kCols * kRed + t * p.parts * kRed + lane;
+                    const float* from = first + t * p.parts * kRed + lane;
                     const float v = p.parts == 2 ? from[0] + from[kRed] : from[0];
                     if (m < a.M) store_as(a.y, (p0 + t) * a.ld_y + m, a.y_type, v);
                 }
@@ -511,13 +516,13 @@ cudaError_t launch_gs4_product(const Gs4Args& a, cudaStream_t st)
     p.a = a;
     p.parts = a.x_type == RMSMP_F32 ? 2 : 1;
     const int64_t expect = a.offsets ? std::max<int64_t>(1, (a.R + a.E - 1) / a.E) : a.R;      // tokens of a matrix
-    // (64 experts of 1408 x 2048, 4 tokens each on average: 35 us eight columns at a time, 40 sixteen; 8 tokens: 51 and 51; 16 tokens: 81 and 71.)
+    // (64 experts of 1408 x 2048, 4 tokens each on average: 35 us eight columns at a time, 40 sixteen; 16 tokens: 81 and 71, and 56 with what chunk_of does.)
     const int nt = expect * p.parts <= 8 ? 1 : 2;
     p.tokens = 8 * nt / p.parts;
     if (!a.offsets) p.tokens = (int)std::min<int64_t>(p.tokens, a.R);
     const int64_t busy = a.offsets ? std::min<int64_t>(a.E, a.R) : 1;                          // matrices with tokens, at most
     const int cols = p.tokens * p.parts, units = a.Kp / 128, sms = a.sms;
-    const size_t ring = (size_t)kWarps * kRing * kChunk * a.block_bytes;
+    const size_t ring = (size_t)kWarps * kRing * chunk_of(nt) * a.block_bytes;
     const size_t column = 2, factor = a.x_type == RMSMP_F16 ? 0 : (size_t)a.sums * 8 * nt * sizeof(float);      // bytes: of an input and column; of 128 inputs
     // Which rows and inputs a warp, a CTA and a cluster take: the least of an estimate in microseconds.  An SM streams 44 KB a microsecond, a warp alone
     // a block in 0.4; x comes in at 40 KB a microsecond; a cluster's join takes 0.7, a second wave of CTAs 1.5.  (8192 x 8192, one bf16 token: 13.1 us with whole
@@ -528,14 +533,14 @@ cudaError_t launch_gs4_product(const Gs4Args& a, cudaStream_t st)
         for (int split = 1; split <= 8 && split <= units; split *= 2) {
             const int wk = kWarps / wr, slice = (units + split - 1) / split;
             const size_t shared_by_all = ring + cols * 64, stage = slice * (128 * column * cols + factor), sums = (size_t)wr * wk * 8 * nt * kRed * sizeof(float);
-            const bool alone = wk == 1 && split == 1 && shared_by_all + sums + stage <= (size_t)kMostSmem;
+            const bool alone = wk == 1 && split == 1 && shared_by_all + sums + stage <= (size_t)kMostSmem, single = alone && nt == 2;      // (only experts have sixteen columns)
             // row blocks of a warp: as many as make one wave
             int64_t rounds = std::max<int64_t>(1, (a.tiles * busy * split + 2 * sms * wr - 1) / (2 * (int64_t)sms * wr));
             if (!alone) rounds = std::min<int64_t>(rounds, 8);
-            if (a.offsets) rounds = 1;                  // (experts' tokens differ: more and shorter CTAs even out)
+            if (a.offsets) rounds = 1;                  // (experts' tokens differ: more and shorter CTAs even out; `single` relies on it)
             rounds = std::min<int64_t>(rounds, (a.tiles + wr - 1) / wr);
             const int per = (int)rounds * wr;
-            const size_t whole = shared_by_all + (alone ? sums : sums * rounds), need = whole + stage;
+            const size_t whole = shared_by_all + (single ? 0 : alone ? sums : sums * rounds), need = whole + stage;
             const int64_t ctas = (a.tiles + per - 1) / per * busy * split, on_sm = (ctas + sms - 1) / sms, at_once = need <= (size_t)kMostSmem / 2 ? 2 : 1;
             const int blocks = (slice + wk - 1) / wk * (int)rounds;
             float t;
@@ -551,7 +556,7 @@ cudaError_t launch_gs4_product(const Gs4Args& a, cudaStream_t st)
             }
             if (t >= best || whole + 128 * column * cols + factor > (size_t)kMostSmem) continue;
             best = t;
-            p.wr = wr; p.wk = wk; p.split = split; p.per = per; p.alone = alone;
+            p.wr = wr; p.wk = wk; p.split = split; p.per = per; p.alone = alone; p.single = single;
             p.groups = (a.tiles + per - 1) / per;
             p.slice = slice * 128;
             p.slab = (int)std::min<int64_t>(p.slice, (int64_t)((kMostSmem - whole) / (128 * column * cols + factor)) * 128);
