@@ -131,14 +131,15 @@ struct Call {
         return p;
     }
     // The same for calls that say so when a tensor is not on the current device: a kernel that is given host memory, or another
-    // GPU's, would fault.  (An int is taken as it is.)  `size`: bytes of its elements, where they can be only one.
+    // GPU's, would fault.  (An int is taken as it is.)  `size`: bytes of its elements, 0 where they may be any; a tensor of narrower ones
+    // than a type code says would be read, or written, past its end.
     long long device = -2;                                      // current device, once asked for
     void* here(int i, long size = 0)
     {
         if (!ok || none(i) || PyLong_Check(a[i])) return ptr(i);
         if (device == -2 && g_device) device = number(PyObject_CallNoArgs(g_device));
-        const long long on = number(PyObject_CallMethodNoArgs(a[i], s_get_device));
-        const long long bytes = size ? number(PyObject_CallMethodNoArgs(a[i], s_element_size)) : 0;
+        const long long on = ok ? number(PyObject_CallMethodNoArgs(a[i], s_get_device)) : -1;
+        const long long bytes = ok && size ? number(PyObject_CallMethodNoArgs(a[i], s_element_size)) : 0;
         if (ok && (on < 0 || (device >= 0 && on != device))) {
             PyErr_SetString(PyExc_ValueError, on < 0 ? "a tensor is not on a CUDA device" : "a tensor is not on the current CUDA device");
             ok = false;
@@ -147,6 +148,12 @@ struct Call {
             ok = false;
         }
         return ptr(i);
+    }
+    // ... of a tensor whose type is argument `type` (another code than these is left to the library to refuse).
+    void* typed(int i, int type)
+    {
+        const int t = i32(type);
+        return here(i, t == RMSMP_F32 ? 4 : t == RMSMP_F16 || t == RMSMP_BF16 ? 2 : 0);
     }
     long long number(PyObject* r)                               // what a method returned
     {
@@ -497,7 +504,7 @@ DEF(gs4_quantize_pack)
     ARGS("rmsmp_gs4_quantize_pack", 4, "layer", "d_W", "w_type", "d_packed", "packed_bytes", "stream")
     void* s = c.stream(5);
     const rmsmp_gs4_layer* L = c.structure<rmsmp_gs4_layer>(0);
-    void* W = c.here(1);
+    void* W = c.typed(1, 2);
     const int type = c.i32(2);
     void* pk = c.here(3);
     const size_t bytes = c.none(4) ? c.bytes_of(3) : c.size(4);
@@ -531,10 +538,10 @@ DEF(gs4_gemm)
     ARGS("rmsmp_gs4_gemm", 9, "layer", "d_packed", "d_x", "x_type", "N", "ld_x", "d_y", "y_type", "ld_y", "stream")
     void* s = c.stream(9);
     const rmsmp_gs4_layer* L = c.structure<rmsmp_gs4_layer>(0);
-    void *pk = c.here(1), *x = c.here(2);
+    void *pk = c.here(1), *x = c.typed(2, 3);
     const int x_type = c.i32(3);
     const long long N = c.i64(4), ld_x = c.i64(5);
-    void* y = c.here(6);
+    void* y = c.typed(6, 7);
     const int y_type = c.i32(7);
     const long long ld_y = c.i64(8);
     RUN("rmsmp_gs4_gemm", api.gs4_gemm(L, pk, x, (rmsmp_dtype)x_type, N, ld_x, y, (rmsmp_dtype)y_type, ld_y, s))
@@ -546,12 +553,12 @@ DEF(gs4_gemm_experts)
     ARGS("rmsmp_gs4_gemm_experts", 12, "layer", "d_packed", "d_x", "x_type", "x_rows", "ld_x", "d_rows", "d_offsets", "R", "d_y", "y_type", "ld_y", "stream")
     void* s = c.stream(12);
     const rmsmp_gs4_layer* L = c.structure<rmsmp_gs4_layer>(0);
-    void *pk = c.here(1), *x = c.here(2);
+    void *pk = c.here(1), *x = c.typed(2, 3);
     const int x_type = c.i32(3);
     const long long x_rows = c.i64(4), ld_x = c.i64(5);
     void *rows = c.here(6, 4), *offsets = c.here(7, 4);
     const long long R = c.i64(8);
-    void* y = c.here(9);
+    void* y = c.typed(9, 10);
     const int y_type = c.i32(10);
     const long long ld_y = c.i64(11);
     RUN("rmsmp_gs4_gemm_experts", api.gs4_gemm_experts(L, pk, x, (rmsmp_dtype)x_type, x_rows, ld_x, (const int32_t*)rows, (const int32_t*)offsets, R, y,
@@ -575,12 +582,12 @@ DEF(expert_gather)
 {
     ARGS("rmsmp_expert_gather", 9, "d_x", "type", "x_rows", "H", "ld_x", "d_rows", "R", "d_xs", "ld_xs", "stream")
     void* s = c.stream(9);
-    void* x = c.here(0);
+    void* x = c.typed(0, 1);
     const int type = c.i32(1);
     const long long x_rows = c.i64(2), H = c.i64(3), ld_x = c.i64(4);
     void* rows = c.here(5, 4);
     const long long R = c.i64(6);
-    void* xs = c.here(7);
+    void* xs = c.typed(7, 1);
     const long long ld_xs = c.i64(8);
     RUN("rmsmp_expert_gather", api.expert_gather(x, (rmsmp_dtype)type, x_rows, H, ld_x, (const int32_t*)rows, R, xs, ld_xs, s))
     Py_RETURN_NONE;
@@ -590,13 +597,13 @@ DEF(expert_combine)
 {
     ARGS("rmsmp_expert_combine", 11, "d_ys", "type", "R", "H", "ld_ys", "d_place", "d_w", "T", "k", "d_y", "ld_y", "stream")
     void* s = c.stream(11);
-    void* ys = c.here(0);
+    void* ys = c.typed(0, 1);
     const int type = c.i32(1);
     const long long R = c.i64(2), H = c.i64(3), ld_ys = c.i64(4);
     void *place = c.here(5, 4), *w = c.here(6, 4);
     const long long T = c.i64(7);
     const int k = c.i32(8);
-    void* y = c.here(9);
+    void* y = c.typed(9, 1);
     const long long ld_y = c.i64(10);
     RUN("rmsmp_expert_combine", api.expert_combine(ys, (rmsmp_dtype)type, R, H, ld_ys, (const int32_t*)place, (const float*)w, T, k, y, ld_y, s))
     Py_RETURN_NONE;
@@ -606,14 +613,14 @@ DEF(expert_combine_backward)
 {
     ARGS("rmsmp_expert_combine_backward", 14, "d_dy", "type", "T", "k", "H", "ld_dy", "d_ys", "R", "ld_ys", "d_place", "d_w", "d_dys", "ld_dys", "d_dw", "stream")
     void* s = c.stream(14);
-    void* dy = c.here(0);
+    void* dy = c.typed(0, 1);
     const int type = c.i32(1);
     const long long T = c.i64(2);
     const int k = c.i32(3);
     const long long H = c.i64(4), ld_dy = c.i64(5);
-    void* ys = c.here(6);
+    void* ys = c.typed(6, 1);
     const long long R = c.i64(7), ld_ys = c.i64(8);
-    void *place = c.here(9, 4), *w = c.here(10, 4), *dys = c.here(11);
+    void *place = c.here(9, 4), *w = c.here(10, 4), *dys = c.typed(11, 1);
     const long long ld_dys = c.i64(12);
     void* dw = c.here(13, 4);
     RUN("rmsmp_expert_combine_backward", api.expert_combine_backward(dy, (rmsmp_dtype)type, T, k, H, ld_dy, ys, R, ld_ys, (const int32_t*)place, (const float*)w,

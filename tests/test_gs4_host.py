@@ -134,6 +134,53 @@ def test_host_tensors_and_other_element_sizes_are_refused_before_the_call():
         R.rmsmp_expert_sort(Ids(), 4, 2, 8, BUF, BUF, BUF, stream=0)
 
 
+class Fake:
+    """A tensor as the binding sees one: on the first device, elements of `size` bytes, an address that no refused call looks at."""
+
+    def __init__(self, size):
+        self.size = size
+
+    def get_device(self): return 0
+    def element_size(self): return self.size
+    def numel(self): return 1 << 20
+    def data_ptr(self): return BUF
+
+
+# every argument whose type is a code beside it: (call, arguments with `x` in its place and `t` in the code's; `bad`: a size that the library refuses)
+TYPED = [
+    ("rmsmp_gs4_quantize_pack", lambda L, x, t, bad: (L, x, t, BUF, 0 if bad else L.packed_bytes)),
+    ("rmsmp_gs4_gemm", lambda L, x, t, bad: (L, BUF, x, t, -1 if bad else 1, 64, BUF, R.F32, 16)),
+    ("rmsmp_gs4_gemm", lambda L, x, t, bad: (L, BUF, BUF, R.F32, -1 if bad else 1, 64, x, t, 16)),
+    ("rmsmp_gs4_gemm_experts", lambda L, x, t, bad: (L, BUF, x, t, 4, 64, BUF, BUF, -1 if bad else 4, BUF, R.F32, 16)),
+    ("rmsmp_gs4_gemm_experts", lambda L, x, t, bad: (L, BUF, BUF, R.F32, 4, 64, BUF, BUF, -1 if bad else 4, x, t, 16)),
+    ("rmsmp_expert_gather", lambda L, x, t, bad: (x, t, 4, 0 if bad else 8, 8, BUF, 4, BUF, 8)),
+    ("rmsmp_expert_gather", lambda L, x, t, bad: (BUF, t, 4, 0 if bad else 8, 8, BUF, 4, x, 8)),
+    ("rmsmp_expert_combine", lambda L, x, t, bad: (x, t, 4, 0 if bad else 8, 8, BUF, BUF, 2, 2, BUF, 8)),
+    ("rmsmp_expert_combine", lambda L, x, t, bad: (BUF, t, 4, 0 if bad else 8, 8, BUF, BUF, 2, 2, x, 8)),
+    ("rmsmp_expert_combine_backward", lambda L, x, t, bad: (x, t, 2, 2, 0 if bad else 8, 8, BUF, 4, 8, BUF, BUF, BUF, 8, BUF)),
+    ("rmsmp_expert_combine_backward", lambda L, x, t, bad: (BUF, t, 2, 2, 0 if bad else 8, 8, x, 4, 8, BUF, BUF, BUF, 8, BUF)),
+    ("rmsmp_expert_combine_backward", lambda L, x, t, bad: (BUF, t, 2, 2, 0 if bad else 8, 8, BUF, 4, 8, BUF, BUF, x, 8, BUF)),
+]
+
+
+@pytest.mark.parametrize("name, args", TYPED, ids=["%s-%d" % (n, i) for i, (n, _) in enumerate(TYPED)])
+@pytest.mark.parametrize("t, size", [(R.F32, 4), (R.F16, 2), (R.BF16, 2)])
+def test_elements_of_another_size_than_their_type_are_refused(name, args, t, size):
+    """A bf16 tensor given as F32 would be read past its end.  (Nothing is launched: every call here is refused, the right size by the library.)"""
+    L = R.rmsmp_gs4_layer_init(1, 16, 64, 32)
+    call = getattr(R, name)
+    for other in (1, 2, 4, 8):
+        if other == size:
+            with pytest.raises(R.RmsmpError) as e:
+                call(*args(L, Fake(size), t, True), stream=0)
+            assert e.value.status in (R.ERR_SHAPE, R.ERR_BUFFER_TOO_SMALL)
+        else:
+            with pytest.raises(ValueError, match="elements"):
+                call(*args(L, Fake(other), t, True), stream=0)
+    with pytest.raises(R.RmsmpError):                   # a code that is no type is the library's to refuse
+        call(*args(L, Fake(4), 7, True), stream=0)
+
+
 # ------------------------------------------------------------------ the oracle itself
 
 @pytest.mark.parametrize("mode", [G.SYM, G.ZERO])
