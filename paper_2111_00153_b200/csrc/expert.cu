@@ -1,6 +1,7 @@
 // Operators on tokens sorted by expert: the order (a stable counting sort of the (token, choice) pairs by expert), the rows copied in that
 // order, the weighted sum back, and its gradient.  The row operators are bound by memory: every row is read and written once.
 #include <algorithm>
+#include <atomic>
 #include "gs4.cuh"
 #include "ptx.cuh"
 
@@ -397,37 +398,49 @@ template <int kType, bool kVec> struct Backward {
     }
 };
 
-cudaError_t sort_with(SortArgs a, cudaStream_t st)
+constexpr int kSortSmem = (kSortWarps + 1) * 1024 * (int)sizeof(uint32_t);      // the most that a CTA takes
+
+// CTAs of the largest cluster that the current device places, asked once: a cluster of sixteen is more than every device promises.  (Threads that
+// ask at the same time each set the attribute before they use it, and store the same answer.)
+int most_sort_ctas()
 {
-    static bool attr_set[kMaxDevices] = {}, large_set[kMaxDevices] = {};
-    a.warps = (int)std::max<uint32_t>(1, std::min<uint32_t>(kSortWarps, (a.P + 32 * a.ctas - 1) / (32 * a.ctas)));
-    const uint32_t warps = (uint32_t)(a.ctas * a.warps);
-    a.per_warp = std::max(1u, (a.P + warps * 32 - 1) / (warps * 32)) * 32;
-    const size_t smem = sizeof(uint32_t) * (a.warps + 1) * (size_t)a.E;
-    const int threads = std::max(a.warps, (a.E + 31) / 32) * 32;           // a thread an expert, and the warps that have pairs
-    if (!ensure_smem_attr(reinterpret_cast<const void*>(expert_sort_kernel), (kSortWarps + 1) * 1024 * 4, attr_set)) return cudaErrorInvalidValue;
-    if (a.ctas == 1) return launch_dependent(expert_sort_kernel, 1, threads, smem, st, a);
-    if (a.ctas > 8) {
-        // (a cluster of sixteen is more than every device promises: where it cannot be had, eight)
-        const int dev = device_ordinal();
-        if (dev >= 0 && !large_set[dev]) {
-            large_set[dev] = true;
-            if (cudaFuncSetAttribute(expert_sort_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) cudaGetLastError();
-        }
+    static std::atomic<int> known[kMaxDevices] = {};
+    const int dev = device_ordinal();
+    if (dev < 0) return 8;
+    int most = known[dev].load(std::memory_order_acquire);
+    if (most) return most;
+    most = 8;
+    if (cudaFuncSetAttribute(expert_sort_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess) {
+        cudaLaunchAttribute at[1];
+        at[0].id = cudaLaunchAttributeClusterDimension;
+        at[0].val.clusterDim.x = 16; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+        cudaLaunchConfig_t lc = {};
+        lc.gridDim = dim3(16); lc.blockDim = dim3(kSortThreads); lc.dynamicSmemBytes = kSortSmem;
+        lc.attrs = at; lc.numAttrs = 1;
+        int clusters = 0;
+        if (cudaOccupancyMaxActiveClusters(&clusters, expert_sort_kernel, &lc) == cudaSuccess && clusters > 0) most = 16;
     }
-    const cudaError_t e = launch_dependent_cluster(expert_sort_kernel, a.ctas, a.ctas, threads, smem, st, a);
-    if (e == cudaSuccess || a.ctas <= 8) return e;
-    a.ctas = 8;
-    return sort_with(a, st);
+    if (most == 8) cudaGetLastError();
+    known[dev].store(most, std::memory_order_release);
+    return most;
 }
 
 }  // namespace
 
 cudaError_t launch_expert_sort(const int32_t* ids, int64_t P, int k, int E, int32_t* offsets, int32_t* rows, int32_t* place, cudaStream_t st)
 {
+    static bool attr_set[kMaxDevices] = {};
+    if (!ensure_smem_attr(reinterpret_cast<const void*>(expert_sort_kernel), kSortSmem, attr_set)) return cudaErrorInvalidValue;
     SortArgs a = {ids, offsets, rows, place, (uint32_t)P, (uint32_t)k, E, 1, 1, 32, 32 - __builtin_clz((unsigned)E)};
     while (a.ctas < 16 && P > (int64_t)a.ctas * kSortThreads * 2) a.ctas *= 2;
-    return sort_with(a, st);
+    if (a.ctas > 8) a.ctas = most_sort_ctas();
+    a.warps = (int)std::max<uint32_t>(1, std::min<uint32_t>(kSortWarps, (a.P + 32 * a.ctas - 1) / (32 * a.ctas)));
+    const uint32_t warps = (uint32_t)(a.ctas * a.warps);
+    a.per_warp = std::max(1u, (a.P + warps * 32 - 1) / (warps * 32)) * 32;
+    const size_t smem = sizeof(uint32_t) * (a.warps + 1) * (size_t)a.E;
+    const int threads = std::max(a.warps, (a.E + 31) / 32) * 32;           // a thread an expert, and the warps that have pairs
+    if (a.ctas == 1) return launch_dependent(expert_sort_kernel, 1, threads, smem, st, a);
+    return launch_dependent_cluster(expert_sort_kernel, a.ctas, a.ctas, threads, smem, st, a);
 }
 
 cudaError_t launch_expert_gather(const void* x, int size, int64_t x_rows, int64_t H, int64_t ld_x, const int32_t* rows, int64_t R, void* xs,
