@@ -457,7 +457,7 @@ rmsmp_status rmsmp_gemm_builtin_scratch(const rmsmp_layer* layer, const void* d_
  * such sum is multiplied by its scale, and those are summed in fp32; the result is rounded once, to y's type.  Codes are exact in every product.  With
  * many tokens activations are too, but for what an fp32 one has below 2^-133.  With few tokens fp16 activations are; a bf16 or fp32 one is first
  * scaled by the power of two that takes the largest of its run to 2^14..2^15, and is then one fp16 number (bf16) or the sum of two (fp32): off by at
- * most 2^-40 of that largest one, and, in fp32, 2^-24 of itself.  (Few: up to eight tokens, four in fp32, and three times that an expert on average.
+ * most 2^-39 of that largest one, and, in fp32, 2^-23 of itself.  (Few: up to eight tokens, four in fp32, and three times that an expert on average.
  * Sums over a run that leave the range of fp32 are infinite.)  The order of the sums follows from sizes, types and alignment: a call repeats bit for bit.
  *
  * Packed buffer: 256-byte header (device status word at byte 64, see rmsmp_last_device_status), then

@@ -154,8 +154,10 @@ __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float(e 
 
 // Inputs k0 .. k0 + slab of `n` rows of x (-1: zeros) into shared memory, a column of `col_bytes` for each part of each token, and the factors
 // ([run][column]).  fp16 goes as it is.  The others are scaled by 2^-e, 2^e <= 2^-14 max|x| < 2^(e+1) over the finite numbers of the run, so that the
-// largest is in 2^14..2^15: a bf16 number's 8 bits are then exact down to 2^-32 of that, where fp16's last place has become fixed.  An fp32 number is the
-// sum of two fp16 ones, each rounded to nearest: 2^-24 of it is left out at most.
+// largest is in 2^14..2^15: a bf16 number's 8 bits are then exact down to 2^-31 of that, where fp16's last place has become fixed; what is smaller is off by
+// half of that place, 2^-25, at most: 2^-39 of the largest.  An fp32 number is the sum of two fp16 ones, each rounded to nearest.  The first leaves up to
+// 2^-11 of it, to a unit of its last place; of 11 bits, the second is off by one such unit at most, 2^-23 of the number.  (A third part would make it
+// exact, for half as many columns again.)
 template <int kSums, int kX>
 __device__ __forceinline__ void stage_x(const Plan& p, uint8_t* xs, float* factors, int columns, uint32_t col_bytes, const int* rows, int n, int k0, int slab)
 {

@@ -358,6 +358,44 @@ def test_fp32_activations_over_their_whole_range():
         assert np.all(np.abs(y - ref) <= tol)
 
 
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("x_name", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("by_expert", [False, True])
+def test_what_few_tokens_keep_of_an_activation(group, x_name, by_expert):
+    """Row m has one code that is not its zero point, at input m, and a scale of one: y is x as the kernel holds it.  fp16 is exact.  The others are off by at
+    most 2^-39 of the largest number of their run (half of fp16's smallest step, 2^-25, beside 2^14), and fp32 by 2^-23 of itself: of a number in 2^e..2^(e+1)
+    the first fp16 part leaves 2^(e-11) at most, which the second, whose half step is 2^-11 of the power of two below that, keeps to 2^(e-12-11)."""
+    import torch
+    size = K = 256
+    codes = np.full((1, size, K), 8, np.uint8)
+    codes[0, np.arange(size), np.arange(K)] = 9
+    layer = R.rmsmp_gs4_layer_init(1, size, K, group, R.GS4_SYM, R.F16)
+    packed = torch.empty(layer.packed_bytes, dtype=torch.uint8, device="cuda")
+    R.rmsmp_gs4_pack_codes(layer, dev(codes), dev(np.ones((1, size, K // group), np.float32), "f16"), None, packed)
+    rng = np.random.default_rng(group)
+    x = rng.standard_normal((4, K)) * 2.0 ** rng.integers(-42, 1, (4, K))      # far below the largest of their run
+    x[1] = 2.0 ** 14 * (1 + rng.random(K))                                     # all in one power of two
+    x[1, ::7] = 2.0 ** 14 + 4 + 2.0 ** -9                                      # the first part's half step, and half of the second's
+    x[2, ::9] = 2.0 ** -39
+    x[2, ::32] = 1.0                                                           # ... beside the largest of every run
+    x[2, 1::11] = 1.0078125 * 2.0 ** -32
+    x[3] = rng.standard_normal(K) * 2.0 ** -130                                # subnormal ones
+    if x_name == "f16":
+        x[1] /= 2
+    dx = dev(x).to(td(x_name))
+    y = torch.empty((4, size), device="cuda")
+    if by_expert:
+        R.rmsmp_gs4_gemm_experts(layer, packed, dx, TYPES[x_name], 4, K, None, dev(np.array([0, 4], np.int32)), 4, y, R.F32, size)
+    else:
+        R.rmsmp_gs4_gemm(layer, packed, dx, TYPES[x_name], 4, K, y, R.F32, size)
+    want, got = host(dx), host(y)
+    run = np.abs(want).reshape(4, -1, min(group, 128)).max(-1).repeat(min(group, 128), axis=1)
+    bound = {"f16": 0.0 * run, "bf16": 2.0 ** -39 * run, "f32": 2.0 ** -39 * run + 2.0 ** -23 * np.abs(want)}[x_name]
+    assert np.all(np.abs(got - want) <= bound)
+    if x_name == "f32":
+        assert np.abs((got - want) / want)[1].max() > 2.0 ** -24               # (and no better: what the header says is what there is)
+
+
 # ------------------------------------------------------------------ experts
 
 def route(seed, T, k, E, padded=0.0, only=None):
