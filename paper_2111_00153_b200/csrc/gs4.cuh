@@ -3,6 +3,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include "common.cuh"
+#include "gs4_plan.h"
 
 namespace rmsmp {
 
@@ -21,6 +22,10 @@ struct Gs4Args {
     int block_bytes, has_zeros;                  // (no zeros: 8 everywhere)
     int scale_bf16, x_type, y_type, x_vec;       // x_vec: rows of x are 16-byte aligned
 };
+inline Gs4Sizes sizes_of(const Gs4Args& a)
+{
+    return {a.R, a.E, a.tiles, a.Kp, a.sums, a.block_bytes, a.x_type, a.offsets != nullptr, !a.rows, a.x_vec != 0, a.sms};
+}
 
 cudaError_t launch_gs4_quantize(const rmsmp_gs4_layer& L, const void* dW, int w_type, uint8_t* blob, cudaStream_t st);
 cudaError_t launch_gs4_pack(const rmsmp_gs4_layer& L, const uint8_t* codes, const void* scale, const uint8_t* zero, uint8_t* blob, cudaStream_t st);

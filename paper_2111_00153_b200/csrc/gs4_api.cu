@@ -71,11 +71,7 @@ rmsmp_status product(const rmsmp_gs4_layer* L, const void* d_packed, const void*
     a.scale_bf16 = L->scale_type == RMSMP_BF16; a.x_type = x_type; a.y_type = y_type;
     a.x_vec = aligned(d_x, 16) && ld_x * dtype_size(x_type) % 16 == 0;
     a.sms = sm_count();
-    // Up to eight columns (an fp32 token is two) by the few-token kernel, more on tcgen05; of experts, which have tiles enough for every SM, up to 24 on average.
-    // (8192 x 8192, 8 and 16 bf16 tokens: 16 and 26 us by the one, 31 and 31 by the other; 4096 x 4096: 9.3 and 11.2, 11.0 and 11.2; 1024 x 1024: 5.1 and 5.6,
-    // 5.2 and 5.2.  64 experts of 1408 x 2048, 16, 24 and 25 tokens each: 56 by the one and 109 by the other, 78 by the one, 96 by the other; eight of 4096 x 4096: 65 and 65, 88 and 66; 256 of 256 x 256, 16: 12 and 30.)
-    const int64_t tokens = experts ? (R + L->E - 1) / L->E : R;
-    const bool many = tokens * (x_type == RMSMP_F32 ? 2 : 1) > (experts ? 24 : 8);
+    const bool many = gs4_many_tokens(R, L->E, x_type, experts);
     return done(many ? launch_gs4_tensor(a, static_cast<cudaStream_t>(stream)) : launch_gs4_product(a, static_cast<cudaStream_t>(stream)));
 }
 

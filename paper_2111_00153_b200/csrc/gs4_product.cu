@@ -11,7 +11,6 @@
 // Weights in turn from more than the L2 holds: 8192 x 8192, one bf16 token 12.4 us, eight fp16 tokens 14.6 (34.9 MB: 2.4 TB/s, 36 % of the measured copy); 65536 x
 // 8192, one token 55 (5.0 TB/s, 77 %).  4096 x 4096, one token 5.7; 1024 x 1024 3.5.  What bounds the large ones is the issue of the expansion beside some 5 us to start, stage
 // x and join; the small ones are that latency alone.  Experts, 64 of 1408 x 2048, 256 pairs: 33 us, 2.9 TB/s: their CTAs do not fill whole waves.
-#include <algorithm>
 #include "gs4.cuh"
 #include "ptx.cuh"
 
@@ -19,23 +18,10 @@ namespace rmsmp {
 
 namespace {
 
-constexpr int kWarps = 8, kThreads = kWarps * 32;
-constexpr int kRing = 2;                 // copies that a warp has in flight or at hand
-// Blocks of a copy.  With sixteen columns, which many short CTAs of experts have, two CTAs fit on an SM if it is one (64 experts of 1408 x 2048, 16 tokens each:
-// 56 us, 70 with two; eight of 4096 x 4096, where one fits at most: 69 and 65); with eight they fit, and more in flight is better (2 tokens each: 21 us, 26 with one).
-__host__ __device__ constexpr int chunk_of(int nt) { return nt == 1 ? 2 : 1; }
-constexpr int kMostSmem = 226 * 1024;
-constexpr int kRed = 36;                 // floats between columns of a block's partial sums (32 rows, padded against bank conflicts)
+constexpr int kWarps = kGs4FewWarps, kThreads = kWarps * 32, kRing = kGs4FewRing, kRed = kGs4FewRed;
 
-struct Plan {
-    Gs4Args a;
-    int wr, wk, split;                   // row blocks x input shares of a CTA's warps; CTAs of a cluster
-    int per, groups;                     // row blocks of a CTA (a multiple of wr); CTAs (clusters) that share a matrix's rows
-    int slice, slab;                     // inputs of a CTA, and of one stage of x in shared memory (multiples of 128)
-    int alone;                           // a warp has all inputs of its row blocks (wk = split = 1, one stage): it stores its sums itself
-    int single;                          // ... of its one row block, sixteen columns: they pass through its ring, which nothing comes into any more
-    int tokens, parts;                   // tokens of one pass over the weights; columns of a token
-};
+struct Operands { Gs4Args a; };
+struct Plan : Operands, Gs4FewPlan {};
 
 // c = a * b + (kFirst ? 0 : c)
 template <bool kFirst>
@@ -270,7 +256,7 @@ __device__ __forceinline__ float ld_cluster(uint32_t addr, int rank)
 template <int kNT, int kSums, bool kZeros, int kX>
 __global__ void __launch_bounds__(kThreads, kNT == 2 ? 2 : 3) gs4_mma_kernel(const __grid_constant__ Plan p)
 {
-    constexpr int kCols = 8 * kNT, kChunk = chunk_of(kNT);
+    constexpr int kCols = 8 * kNT, kChunk = gs4_few_chunk(kNT);
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ __align__(8) uint64_t s_full[kWarps][kRing];
     __shared__ int s_abort, s_found[3];
@@ -487,30 +473,30 @@ __global__ void __launch_bounds__(kThreads, kNT == 2 ? 2 : 3) gs4_mma_kernel(con
 }
 
 template <int kNT, int kSums, bool kZeros, int kX>
-cudaError_t launch_one(const Plan& p, int64_t grid, size_t smem, cudaStream_t st)
+cudaError_t launch_one(const Plan& p, cudaStream_t st)
 {
     static bool attr_set[kMaxDevices] = {};
     auto* const kernel = gs4_mma_kernel<kNT, kSums, kZeros, kX>;
-    if (!ensure_smem_attr(reinterpret_cast<const void*>(kernel), kMostSmem, attr_set)) return cudaErrorInvalidValue;
-    if (p.split == 1) return launch_dependent(kernel, (unsigned)grid, kThreads, smem, st, p);
-    return launch_dependent_cluster(kernel, p.split, (unsigned)grid, kThreads, smem, st, p);
+    if (!ensure_smem_attr(reinterpret_cast<const void*>(kernel), kGs4MostSmem, attr_set)) return cudaErrorInvalidValue;
+    if (p.split == 1) return launch_dependent(kernel, (unsigned)p.grid, kThreads, p.smem, st, p);
+    return launch_dependent_cluster(kernel, p.split, (unsigned)p.grid, kThreads, p.smem, st, p);
 }
 template <int kNT, int kSums, bool kZeros>
-cudaError_t launch_type(const Plan& p, int64_t grid, size_t smem, cudaStream_t st)
+cudaError_t launch_type(const Plan& p, cudaStream_t st)
 {
-    return p.a.x_type == RMSMP_F16    ? launch_one<kNT, kSums, kZeros, RMSMP_F16>(p, grid, smem, st)
-           : p.a.x_type == RMSMP_BF16 ? launch_one<kNT, kSums, kZeros, RMSMP_BF16>(p, grid, smem, st)
-                                      : launch_one<kNT, kSums, kZeros, RMSMP_F32>(p, grid, smem, st);
+    return p.a.x_type == RMSMP_F16    ? launch_one<kNT, kSums, kZeros, RMSMP_F16>(p, st)
+           : p.a.x_type == RMSMP_BF16 ? launch_one<kNT, kSums, kZeros, RMSMP_BF16>(p, st)
+                                      : launch_one<kNT, kSums, kZeros, RMSMP_F32>(p, st);
 }
 template <int kNT, int kSums>
-cudaError_t launch_kind(const Plan& p, int64_t grid, size_t smem, cudaStream_t st)
+cudaError_t launch_kind(const Plan& p, cudaStream_t st)
 {
-    return p.a.has_zeros ? launch_type<kNT, kSums, true>(p, grid, smem, st) : launch_type<kNT, kSums, false>(p, grid, smem, st);
+    return p.a.has_zeros ? launch_type<kNT, kSums, true>(p, st) : launch_type<kNT, kSums, false>(p, st);
 }
 template <int kNT>
-cudaError_t launch_sums(const Plan& p, int64_t grid, size_t smem, cudaStream_t st)
+cudaError_t launch_sums(const Plan& p, cudaStream_t st)
 {
-    return p.a.sums == 1 ? launch_kind<kNT, 1>(p, grid, smem, st) : p.a.sums == 2 ? launch_kind<kNT, 2>(p, grid, smem, st) : launch_kind<kNT, 4>(p, grid, smem, st);
+    return p.a.sums == 1 ? launch_kind<kNT, 1>(p, st) : p.a.sums == 2 ? launch_kind<kNT, 2>(p, st) : launch_kind<kNT, 4>(p, st);
 }
 
 }  // namespace
@@ -518,57 +504,10 @@ cudaError_t launch_sums(const Plan& p, int64_t grid, size_t smem, cudaStream_t s
 cudaError_t launch_gs4_product(const Gs4Args& a, cudaStream_t st)
 {
     Plan p;
+    static_cast<Gs4FewPlan&>(p) = gs4_plan_few(sizes_of(a));
     p.a = a;
-    p.parts = a.x_type == RMSMP_F32 ? 2 : 1;
-    const int64_t expect = a.offsets ? std::max<int64_t>(1, (a.R + a.E - 1) / a.E) : a.R;      // tokens of a matrix
-    // (64 experts of 1408 x 2048, 4 tokens each on average: 35 us eight columns at a time, 40 sixteen; 16 tokens: 81 and 71, and 56 with what chunk_of does.)
-    const int nt = expect * p.parts <= 8 ? 1 : 2;
-    p.tokens = 8 * nt / p.parts;
-    if (!a.offsets) p.tokens = (int)std::min<int64_t>(p.tokens, a.R);
-    const int64_t busy = a.offsets ? std::min<int64_t>(a.E, a.R) : 1;                          // matrices with tokens, at most
-    const int cols = p.tokens * p.parts, units = a.Kp / 128, sms = a.sms;
-    const size_t ring = (size_t)kWarps * kRing * chunk_of(nt) * a.block_bytes;
-    const size_t column = 2, factor = a.x_type == RMSMP_F16 ? 0 : (size_t)a.sums * 8 * nt * sizeof(float);      // bytes: of an input and column; of 128 inputs
-    // Which rows and inputs a warp, a CTA and a cluster take: the least of an estimate in microseconds.  An SM streams 44 KB a microsecond, a warp alone a block in
-    // 0.4; a CTA takes 4 to start, find its tokens and end, x comes in at 10 KB a microsecond, behind the weights' first copies, a cluster's join takes 2.
-    // (8192 x 8192, one bf16 token: 13.1 us with whole rows a CTA, 12.7 with quarters; 1024 x 1024: 3.5 and 4.3; eight tokens, 16384 x 8192: quarters 22.9 us, halves 24.6, whole
-    // rows 37; 32768 x 4096: whole rows 25, eighths with several row blocks a warp 56.  64 experts of 1408 x 2048, 4 tokens each: eight row blocks a CTA 33 us,
-    // four 35, two 46; 8 tokens of 8: two 8.3, four 8.0, eight 11; eight experts of 4096 x 4096, 4 tokens: 24.3, halved in a cluster 23.4.)
-    size_t smem = 0;
-    float best = 1e30f;
-    for (int wr = 1; wr <= kWarps; wr *= 2)
-        for (int split = 1; split <= 8 && split <= units; split *= 2) {
-            const int wk = kWarps / wr, slice = (units + split - 1) / split;
-            const size_t shared_by_all = ring + cols * 64, stage = slice * (128 * column * cols + factor), sums = (size_t)wr * wk * 8 * nt * kRed * sizeof(float);
-            const bool alone = wk == 1 && split == 1 && shared_by_all + sums + stage <= (size_t)kMostSmem, single = alone && nt == 2;      // (only experts have sixteen columns)
-            // Row blocks of a warp: as many as make one wave, half of them, or one.  (Experts' tokens differ: more and shorter CTAs even out; `single` relies on it.)
-            int64_t most = a.offsets ? 1 : std::max<int64_t>(1, (a.tiles * split + 2 * sms * wr - 1) / (2 * (int64_t)sms * wr));
-            if (!alone) most = std::min<int64_t>(most, 8);
-            most = std::min<int64_t>(most, (a.tiles + wr - 1) / wr);
-            for (int64_t rounds = most; rounds > 0; rounds = rounds == 1 ? 0 : rounds == most ? (most + 1) / 2 : 1) {
-                const int per = (int)rounds * wr;
-                const size_t whole = shared_by_all + (single ? 0 : alone ? sums : sums * rounds), need = whole + stage;
-                const int64_t ctas = (a.tiles + per - 1) / per * busy * split, at_once = need <= (size_t)kMostSmem / 2 ? 2 : 1;
-                const int blocks = (slice + wk - 1) / wk * (int)rounds;
-                // (waves: whole ones; of experts, whose CTAs differ, as many as they fill and half a one for the last)
-                const int64_t slots = at_once * sms * (split >= 4 ? 7 : 8) / 8;         // (clusters of four and eight leave SMs over)
-                const float full = (float)ctas / slots, block_us = std::max(0.4f, std::min(1.0f, full) * at_once * kWarps * (a.block_bytes / 44e3f));
-                const float waves = full <= 1 ? 1.0f : a.offsets ? full + 0.5f : (float)((ctas + slots - 1) / slots);
-                const float t = waves * (blocks * block_us + 4.0f + slice * 256e-4f * std::min<int64_t>(p.tokens, expect) * p.parts + (split > 1 ? 2.0f : 0.0f));
-                if (t >= best || whole + 128 * column * cols + factor > (size_t)kMostSmem) continue;
-                best = t;
-                p.wr = wr; p.wk = wk; p.split = split; p.per = per; p.alone = alone; p.single = single;
-                p.groups = (a.tiles + per - 1) / per;
-                p.slice = slice * 128;
-                p.slab = (int)std::min<int64_t>(p.slice, (int64_t)((kMostSmem - whole) / (128 * column * cols + factor)) * 128);
-                smem = whole + p.slab * column * cols + p.slab / 128 * factor;
-            }
-        }
-    // Passes over the weights: a matrix's last is not full.  (All of 512 tokens with one of 64 experts of 1408 x 2048: 40 us, by CTAs that each go through
-    // all of a matrix's tokens 589; where experts have 0 to 14 each, 35.6 and 42.9.)  CTAs behind the last pass there is find nothing to do.
-    const int64_t passes = a.offsets ? busy + (a.R - busy) / p.tokens : 1, grid = passes * p.groups * p.split;
-    if (grid > (1ll << 31) - 1) return cudaErrorInvalidValue;
-    return nt == 1 ? launch_sums<1>(p, grid, smem, st) : launch_sums<2>(p, grid, smem, st);
+    if (p.grid > (1ll << 31) - 1) return cudaErrorInvalidValue;
+    return p.nt == 1 ? launch_sums<1>(p, st) : launch_sums<2>(p, st);
 }
 
 }  // namespace rmsmp

@@ -27,7 +27,6 @@ namespace {
 
 constexpr int kWorkers = 512, kWorkWarps = kWorkers / 32;
 constexpr int kIssuer = kWorkWarps, kCopier = kWorkWarps + 1;         // the warp that issues matrix instructions; the one that issues copies of x
-constexpr int kMostSmem = 226 * 1024;
 constexpr int kBytesA = 128 * 128 * 2;                    // operand A of 128 inputs: two tiles of 128 rows x 64 inputs
 constexpr int kOutPad = 4;                                // floats behind a token's 128 sums in shared memory
 
@@ -556,7 +555,7 @@ template <int kBN, int kX, bool kBulk>
 cudaError_t launch_one(Plan& p, cudaStream_t st)
 {
     static bool attr_set[kMaxDevices] = {};
-    constexpr int kRoom = kMostSmem - 12 * kBN - 768;               // beside the static shared memory
+    constexpr int kRoom = kGs4MostSmem - 12 * kBN - 768;               // beside the static shared memory
     auto* const kernel = gs4_tensor_kernel<kBN, kX, kBulk>;
     if (!ensure_smem_attr(reinterpret_cast<const void*>(kernel), kRoom, attr_set)) return cudaErrorInvalidValue;
     const size_t fixed = 1024 + 2 * kBytesA + (size_t)kStagesB<kBN, kX> * kBytesB<kBN, kX>, slot = 4 * (size_t)p.a.block_bytes;
@@ -595,35 +594,15 @@ cudaError_t launch_tokens(Plan& p, int bn, cudaStream_t st)
 
 cudaError_t launch_gs4_tensor(const Gs4Args& a, cudaStream_t st)
 {
+    const Gs4ManyPlan of = gs4_plan_many(sizes_of(a));
+    if (of.ntiles > (1 << 30)) return cudaErrorInvalidValue;
     Plan p;
     p.a = a;
-    p.mtiles = (a.tiles + 3) / 4;
-    const int units = a.Kp / 128;
-    const int64_t expect = a.offsets ? std::max<int64_t>(1, (a.R + a.E - 1) / a.E) : a.R;      // tokens of a matrix
-    const int64_t busy = a.offsets ? std::min<int64_t>(a.E, a.R) : 1;
-    // Tokens of a tile and CTAs of a cluster: the least of an estimate.  A CTA takes `pace` microseconds for 128 inputs (measured: 4096 x 4096; `bulk`: x by tensor
-    // copies), 2.5 to start and to end, a cluster's join another; every SM has one CTA.
-    static constexpr struct { int bn; float pace, bulk; } kTiles[] = {{16, 0.75f, 0.72f}, {32, 0.78f, 0.75f}, {64, 0.83f, 0.8f}, {128, 1.05f, 0.95f}, {192, 1.35f, 1.07f}, {256, 1.7f, 1.25f}};
-    const bool bulk = !a.rows && a.x_vec;
-    float best = 1e30f;
-    int bn = 16;
-    for (const auto& tile : kTiles) {
-        if (tile.bn > 64 && a.x_type == RMSMP_F32) break;
-        // (experts' last tiles are half empty on average)
-        const float per = a.offsets ? std::max(1.0f, (float)expect / tile.bn + 0.5f) : (float)((expect + tile.bn - 1) / tile.bn);
-        const int64_t tiles = (int64_t)(busy * per * p.mtiles);
-        for (int split = 1; split <= 4 && split <= units; split *= 2) {         // (clusters of eight wait for room: 1024 x 1024, 32 tokens 10.9 us, fours 5.5)
-            const float t = (float)((tiles * split + a.sms - 1) / a.sms) * ((units + split - 1) / split * (bulk ? tile.bulk : tile.pace) * (a.x_type == RMSMP_F32 ? 1.8f : 1.0f) + 2.5f + (split > 1 ? 1.0f : 0.0f));
-            if (t < best) { best = t; bn = tile.bn; p.split = split; }
-        }
-        if (tile.bn >= (a.offsets ? 4 : 1) * expect) break;
-    }
-    const int64_t ntiles = (a.R + bn - 1) / bn + (a.offsets ? std::min<int64_t>(a.E, a.R) : 0);
-    if (ntiles > (1 << 30)) return cudaErrorInvalidValue;
-    p.ntiles = (int)ntiles;
-    p.units = (units + p.split - 1) / p.split;
+    p.split = of.split; p.units = of.units; p.mtiles = of.mtiles; p.ntiles = (int)of.ntiles;
     p.y_vec = (reinterpret_cast<uintptr_t>(a.y) % (4 * dtype_size(a.y_type))) == 0 && a.ld_y % 4 == 0;
-    return a.x_type == RMSMP_F16 ? launch_tokens<RMSMP_F16>(p, bn, st) : a.x_type == RMSMP_BF16 ? launch_tokens<RMSMP_BF16>(p, bn, st) : launch_tokens<RMSMP_F32>(p, bn, st);
+    return a.x_type == RMSMP_F16    ? launch_tokens<RMSMP_F16>(p, of.bn, st)
+           : a.x_type == RMSMP_BF16 ? launch_tokens<RMSMP_BF16>(p, of.bn, st)
+                                    : launch_tokens<RMSMP_F32>(p, of.bn, st);
 }
 
 }  // namespace rmsmp
