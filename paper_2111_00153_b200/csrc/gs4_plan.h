@@ -88,7 +88,7 @@ inline Gs4FewPlan gs4_plan_few(const Gs4Sizes& a)
                 const int64_t ctas = (a.tiles + per - 1) / per * busy * split, at_once = need <= (size_t)kGs4MostSmem / 2 ? 2 : 1;
                 const int blocks = (slice + wk - 1) / wk * (int)rounds;
                 // (waves: whole ones; of experts, whose CTAs differ, as many as they fill and half a one for the last)
-                const int64_t slots = at_once * sms * (split >= 4 ? 7 : 8) / 8;         // (clusters of four and eight leave SMs over)
+                const int64_t slots = std::max<int64_t>(1, at_once * sms * (split >= 4 ? 7 : 8) / 8);      // (clusters of four and eight leave SMs over)
                 const float full = (float)ctas / slots, block_us = std::max(0.4f, std::min(1.0f, full) * at_once * kGs4FewWarps * (a.block_bytes / 44e3f));
                 const float waves = full <= 1 ? 1.0f : a.experts ? full + 0.5f : (float)((ctas + slots - 1) / slots);
                 const float t = waves * (blocks * block_us + 4.0f + slice * 256e-4f * std::min<int64_t>(p.tokens, expect) * p.parts + (split > 1 ? 2.0f : 0.0f));

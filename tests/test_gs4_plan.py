@@ -4,6 +4,7 @@ import ctypes as C
 import os
 import random
 import subprocess
+import sys
 
 import pytest
 
@@ -67,6 +68,24 @@ def test_plans_are_sound(plan):
             # passes: what any spread of R rows over E matrices can need
             most = max(sum(-(-n // p["tokens"]) for n in spread) for spread in ([R], [1] * (min(E, R) - 1) + [R - min(E, R) + 1])) if experts else 1
             assert p["grid"] >= most * p["groups"] * p["split"]
+
+
+def test_plans_of_a_device_whose_sms_are_not_known(tmp_path):
+    """Counted as one: seven eighths of that, which clusters are given, were none, and the division by them ended the process.  (So in a process of its own.)"""
+    lib = str(tmp_path / "gs4_plan.so")
+    subprocess.check_call(["g++", "-std=c++17", "-O2", "-shared", "-fPIC", SOURCE, "-o", lib])
+    code = """
+import ctypes as C, sys
+lib = C.CDLL(sys.argv[1])
+lib.gs4_few.argtypes = [C.c_int64] + [C.c_int] * 10 + [C.POINTER(C.c_int64)]
+out = (C.c_int64 * %d)()
+for experts, E in ((0, 1), (1, 5)):
+    for sms in (1, 2):
+        lib.gs4_few(8, E, 4096, 4096, 64, 1, 1, experts, 1, 1, sms, out)
+        print(out[0], out[3])
+""" % len(S.FEW)
+    done = subprocess.run([sys.executable, "-c", code, lib], capture_output=True, text=True, timeout=60)
+    assert done.returncode == 0 and len(done.stdout.split()) == 8
 
 
 def test_the_tested_shapes_take_every_form(plan):
