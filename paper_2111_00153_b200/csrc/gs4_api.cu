@@ -65,7 +65,8 @@ rmsmp_status product(const rmsmp_gs4_layer* L, const void* d_packed, const void*
     Gs4Args a = {};
     a.blocks = blob + L->off_blocks; a.block_bytes = L->block_bytes; a.has_zeros = L->mode == RMSMP_GS4_ZERO;
     a.status = reinterpret_cast<uint32_t*>(const_cast<uint8_t*>(blob) + kStatusOffset);
-    a.x = d_x; a.y = d_y; a.rows = d_rows; a.offsets = d_offsets;
+    a.x = x_rows ? d_x : d_packed;               // (no rows: a copy of no bytes still names an address, and that of d_x may be null)
+    a.y = d_y; a.rows = d_rows; a.offsets = d_offsets;
     a.x_rows = x_rows; a.ld_x = ld_x; a.ld_y = ld_y; a.R = R;
     a.M = L->M; a.K = L->K; a.Kp = L->Kp; a.tiles = L->tiles; a.E = L->E; a.sums = L->sums;
     a.scale_bf16 = L->scale_type == RMSMP_BF16; a.x_type = x_type; a.y_type = y_type;

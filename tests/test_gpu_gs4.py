@@ -276,6 +276,21 @@ def test_rows_of_x_that_are_not_there():
                         check_close(out[q:q + 1], ref, absum, x_name, 52)
 
 
+@pytest.mark.parametrize("x_name", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("Rn", [6, 120])
+@pytest.mark.parametrize("by_rows", [True, False])
+def test_x_without_any_rows(x_name, Rn, by_rows):
+    """No rows of x, and no address either: every row that has an expert is zeros, few and many of them."""
+    import torch
+    p = Packed(2, 2, 70, 256, 64, R.GS4_ZERO)
+    y = torch.full((Rn, 70), float("nan"), dtype=td(x_name), device="cuda")
+    index = torch.arange(Rn, dtype=torch.int32, device="cuda") if by_rows else None
+    R.rmsmp_gs4_gemm_experts(p.layer, p.packed, None, TYPES[x_name], 0, 256, index, dev(np.array([1, Rn // 3, Rn - 1], np.int32)), Rn, y, TYPES[x_name], 70)
+    torch.cuda.synchronize()
+    assert R.rmsmp_last_device_status(p.packed) == R.OK
+    assert (y[1:-1] == 0).all() and torch.isnan(y[0]).all() and torch.isnan(y[-1]).all()
+
+
 def test_two_streams_at_once():
     """The same layer on two streams, many tokens on one and few on the other, again and again: nothing is shared but the weights."""
     import torch
