@@ -567,7 +567,8 @@ rmsmp_status rmsmp_expert_combine(const void* d_ys, rmsmp_dtype type, int64_t R,
 /*
  * The gradient of rmsmp_expert_combine: dys[d_place[t][j]] = w[t][j] * dy[t] and dw[t][j] = <dy[t], ys[d_place[t][j]]> (fp32 sums, a fixed order).
  * A pair without a place has dw = 0; rows of dys that no pair has are left as they were.  d_w NULL: ones.  d_dys or d_dw may be NULL if not
- * wanted (not both; d_ys may be NULL without d_dw).  Two pairs with one place, which rmsmp_expert_sort never gives, leave one of their rows.
+ * wanted (not both; d_ys may be NULL without d_dw).  Places of two pairs differ, as rmsmp_expert_sort's do: where they do not, each value of that row of
+ * dys is that of one of the pairs, not the same one's for the whole row or from call to call (dw is not concerned).
  * Errors: as rmsmp_expert_gather.
  */
 rmsmp_status rmsmp_expert_combine_backward(const void* d_dy, rmsmp_dtype type, int64_t T, int k, int64_t H, int64_t ld_dy,

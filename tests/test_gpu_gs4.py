@@ -571,6 +571,26 @@ def test_combine_backward(T, k, E, H, pad, name, padded):
             assert float(dwb[0]) == -9.0 and float(dwb[-1]) == -9.0
 
 
+@pytest.mark.parametrize("H", [8, 777, 2048])
+def test_pairs_that_share_a_place(H):
+    """Each value of the row is one of those pairs'; dw is right for all of them, and no other row is touched."""
+    import torch
+    T, k, P = 40, 2, 9
+    rng = np.random.default_rng(H)
+    dy, ys = rng.standard_normal((T, H)).astype(np.float32), rng.standard_normal((P, H)).astype(np.float32)
+    place = np.full((T, k), -1, np.int32)
+    place[:, 1] = 5
+    place[3] = (7, 7)                                   # ... and twice by one token
+    dys, dw = torch.full((P, H), float("nan"), device="cuda"), torch.empty((T, k), device="cuda")
+    R.rmsmp_expert_combine_backward(dev(dy), R.F32, T, k, H, H, dev(ys), P, H, dev(place), None, dys, H, dw)
+    _, dw_ref, absum = G.combine_backward(dy, ys, place, None)
+    check_close(host(dw), dw_ref, absum, "f32", H / 16 + 24, 2.0 ** -24)
+    out = host(dys)
+    others = np.delete(dy, 3, 0)
+    assert (out[5][None] == others).any(0).all() and np.array_equal(out[7], dy[3])
+    assert np.isnan(np.delete(out, (5, 7), 0)).all()
+
+
 def test_gradients_against_differences():
     """The sum is linear in the rows and in the weights: differences of the call itself give its gradient up to rounding."""
     import torch
