@@ -484,7 +484,7 @@ typedef struct rmsmp_gs4_layer {
 
 /*
  * Describe E matrices of M rows and K inputs.  Host only.  Limits: 1 <= E <= 4096, 1 <= M, K <= 2^20, group a multiple of 32 in
- * 32..2^20 (it may exceed K: one scale a row; the last group of a row may be cut short).  Errors: NULL, SHAPE, SCHEME (mode, scale_type).
+ * 32..2^20 (it may exceed K: one scale a row; the last group of a row may be cut short).  (rmsmp_expert_sort knows 1024 experts at most.)  Errors: NULL, SHAPE, SCHEME (mode, scale_type).
  */
 rmsmp_status rmsmp_gs4_layer_init(rmsmp_gs4_layer* layer, int E, int M, int K, int group, rmsmp_gs4_mode mode,
                                   rmsmp_dtype scale_type);

@@ -151,7 +151,7 @@ __global__ void __launch_bounds__(kSortThreads) expert_sort_kernel(const SortArg
 
 // ------------------------------------------------------------------ rows
 // Rows whose pieces of 16 bytes are aligned everywhere are read and written in those; others value by value (8192 tokens of two choices, 1001 fp16 columns: gather 24 us
-// for 66 MB, combine 35; 1024 columns go at the rates given below).
+// for 66 MB, combine 35, on another card 27 and 38; 1024 columns 10 and 11).
 constexpr int kRowThreads = 256;
 
 // Rows are cut into pieces of kBytes; a block's threads are `rows` rows x `lanes` pieces.
@@ -247,7 +247,8 @@ struct CombineArgs {
 
 // y[t] = sum_j w[t][j] ys[place[t][j]].  `lanes` threads a token, a piece each; kTerms: choices whose rows a thread reads at once.  Bound by memory: 8192 tokens of eight
 // choices and 2048 bf16 columns, a tenth without a place: 45 us, 6.1 TB/s, 93 % of the measured copy.  As many blocks an SM as leave each thread the registers for its rows
-// (16384 tokens of four choices: 57 us with five, 87 with eight; of two 39 with six, 56 with eight; 4096 of eight, eight rows at once 26 us, four 26, two 28, one 31).
+// (16384 tokens of four choices: 57 us with five, 87 with eight; of two 39 with six, 56 with eight; 4096 of eight, eight rows at once 26 us, four 26, two 28, one 31;
+// at these bounds ptxas spills one to six words of the 16-bit forms of one, two and eight).
 template <int kType, bool kVec, int kTerms>
 __global__ void __launch_bounds__(kRowThreads, kTerms == 8 ? 4 : kTerms == 4 ? 5 : kTerms == 2 ? 6 : 8) expert_combine_kernel(const CombineArgs a)
 {
@@ -289,6 +290,7 @@ __global__ void __launch_bounds__(kRowThreads, kTerms == 8 ? 4 : kTerms == 4 ? 5
 // dys[place[t][j]] = w[t][j] dy[t], dw[t][j] = <dy[t], ys[place[t][j]]>.  `lanes` threads a token, at most a warp's (kBlock: all of a block's): dy is read once for kTerms
 // choices, whose rows are read together; the dot products meet by shuffles, and in shared memory, in a fixed order.  Bound by memory: 4096 tokens of eight
 // choices and 2048 bf16 columns 51 us, 5.6 TB/s, 86 % of the measured copy (choices one by one 63 us, two at once 51, four 49).
+// (ptxas spills one to six words of the forms in whole pieces with less than a block a token: of one choice, and of two in fp32.)
 template <int kType, bool kVec, bool kBlock, int kTerms>
 __global__ void __launch_bounds__(kRowThreads, !kVec ? 3 : kTerms >= 4 ? 4 : 6) expert_combine_backward_kernel(const CombineArgs a)
 {

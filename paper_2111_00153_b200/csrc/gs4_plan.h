@@ -27,7 +27,8 @@ constexpr int kGs4MostSmem = 226 * 1024;
 // ---- which kernel
 // Up to eight columns (an fp32 token is two) by the few-token kernel, more on tcgen05; of experts, which have tiles enough for every SM, up to 24 on average.
 // (8192 x 8192, 8 and 16 bf16 tokens: 16 and 26 us by the one, 31 and 31 by the other; 4096 x 4096: 9.3 and 11.2, 11.0 and 11.2; 1024 x 1024: 5.1 and 5.6,
-// 5.2 and 5.2.  64 experts of 1408 x 2048, 16, 24 and 25 tokens each: 56 by the one and 109 by the other, 78 by the one, 96 by the other; eight of 4096 x 4096: 65 and 65, 88 and 66; 256 of 256 x 256, 16: 12 and 30.)
+// 5.2 and 5.2.  64 experts of 1408 x 2048, 16, 24 and 25 tokens each: 56 by the one and 109 by the other, 78 by the one, 96 by the other; eight of 4096 x 4096: 65 and 65, 88 and 66; 256 of 256 x 256, 16: 12 and 30.
+// One number of columns for all sizes takes the slower of the two for 9 to 16 tokens of 8192 x 8192, and for 17 to 24 an expert of eight large ones.)
 inline bool gs4_many_tokens(int64_t R, int E, int x_type, bool experts)
 {
     const int64_t tokens = experts ? (R + E - 1) / E : R;

@@ -3,14 +3,16 @@
 // The inner sums are warp-level matrix instructions of 16 rows x 8 columns x 16 inputs on fp16 numbers with fp32 sums: a code becomes its exact
 // fp16 integer by five logic operations and four half2 additions for eight codes, and the CUDA cores have no multiply-add of their own but those
 // by the scale.  (fp16 whatever the activations' type: in bf16, whose last place is 1 at 128 where fp16's is 1 at 1024, every pair of codes
-// needs a shift of its own, 7 logic operations for eight; at half rate they are what bounds an SM.)  Columns are tokens; bf16 and fp32
+// needs a shift of its own, 7 logic operations for eight, which go at half rate.)  Columns are tokens; bf16 and fp32
 // activations come to fp16 by a power of two for every run and token, an fp32 one as two columns (see stage_x).
 // A warp streams blocks of 32 rows x 128 inputs (2 KB of codes) through a ring of its own in shared memory, filled by bulk copies; a CTA's warps are
 // `wr` row blocks x `wk` shares of the inputs, each CTA has `per` row blocks, and a cluster of `split` CTAs shares the inputs further where there are
 // few rows.  Partial sums meet in shared memory, and across the cluster in distributed shared memory, in a fixed order; no scratch memory, no atomics.
-// Weights in turn from more than the L2 holds: 8192 x 8192, one bf16 token 12.4 us, eight fp16 tokens 14.6 (34.9 MB: 2.4 TB/s, 36 % of the measured copy); 65536 x
-// 8192, one token 55 (5.0 TB/s, 77 %).  4096 x 4096, one token 5.7; 1024 x 1024 3.5.  What bounds the large ones is the issue of the expansion beside some 5 us to start, stage
-// x and join; the small ones are that latency alone.  Experts, 64 of 1408 x 2048, 256 pairs: 33 us, 2.9 TB/s: their CTAs do not fill whole waves.
+// Weights in turn from more than the L2 holds (ranges: several cards): 8192 x 8192, one bf16 token 12.4 to 13.1 us, eight fp16 tokens 14.6 to 15.9 (34.9 MB: 2.2 to 2.4 TB/s, a
+// third of the measured copy), eight bf16 16 to 17.4, one fp32 16, four 17; 65536 x 8192, one token 55 to 59 (4.7 to 5.0 TB/s, 73 to 77 %).  4096 x 4096, one token 5.7 to 6.4;
+// 1024 x 1024 3.5 to 4.4.  What bounds them is latency: for eight tokens of 8192 x 8192 an SM issues 1.24 instructions a cycle of four, the tensor pipe is busy for 10 % and
+// DRAM for 23 %.  An SM reads 234 KB of its codes, under four fills of its rings, so the start, staging x (all of a CTA's inputs, ahead of its first block: some 3 of the 15 us by the rate in gs4_plan.h) and the join are
+// what is measured.  Experts, 64 of 1408 x 2048, 256 pairs: 33 to 36 us, 2.7 to 2.9 TB/s: their CTAs do not fill whole waves.
 #include "gs4.cuh"
 #include "ptx.cuh"
 
@@ -153,7 +155,7 @@ __device__ __forceinline__ void stage_x(const Plan& p, uint8_t* xs, float* facto
     const int lg = min(32 - __clz(vecs - 1), 31 - __clz(kThreads));             // 2^lg threads a token; 16 vectors a block, so 16 lanes go through this together
     const int v0 = threadIdx.x & ((1 << lg) - 1);
     int t_next = v0 < vecs ? threadIdx.x >> lg : n, v_next = v0;
-        constexpr int kAhead = 2;                             // vectors that a thread has under way (4096 x 4096, eight tokens: 9.1 us, one by one 9.5)
+    constexpr int kAhead = 2;                                 // vectors that a thread has under way (4096 x 4096, eight tokens: 9.1 us, one by one 9.5)
     while (t_next < n) {
         int ts[kAhead], vs[kAhead];
         uint32_t ws[kAhead][4 * kParts];
@@ -253,6 +255,8 @@ __device__ __forceinline__ float ld_cluster(uint32_t addr, int rank)
     return v;
 }
 
+// (At these bounds, 128 registers with sixteen columns and 80 with eight, ptxas spills two words in ten forms: those of fp32 and bf16 with sixteen columns and two or four runs, and with
+// eight columns, four runs and no zeros.)
 template <int kNT, int kSums, bool kZeros, int kX>
 __global__ void __launch_bounds__(kThreads, kNT == 2 ? 2 : 3) gs4_mma_kernel(const __grid_constant__ Plan p)
 {

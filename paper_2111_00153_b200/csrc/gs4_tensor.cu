@@ -15,7 +15,8 @@
 // shared memory and copies 26 %, L2 14 %).  Tried against that: pairs of CTAs that share operand B (cta_group::2, 256 rows: every block waits for the other CTA,
 // 63 us); operand A in tensor memory (no room for two accumulators of 256 tokens; 192: 39 us for 768 tokens, 41 this way); a warp of its own for the copies of
 // codes, and their slots free before the sums are taken (46 us); blocks of inputs in another order for every CTA (48 us: CTAs that read the same x at the same time
-// share their reads).  With few tokens it is the expansion, some 600 cycles a block.
+// share their reads).  With few tokens a tile it is the expansion, some 600 cycles a block whatever their number: 8192 x 8192, 9 to 64 tokens 31 to 36 us (floor 5.4), 4096 x 4096, 64 tokens
+// 12 to 13 (1.5).  fp32: tiles of 64 tokens at most, whose x every row tile's CTAs split again: 4096 x 4096, 512 tokens 123 us, 140 TFLOP/s; 4096 x 1024, 2048 tokens 129.
 #include <algorithm>
 #include "gs4.cuh"
 #include "ptx.cuh"
@@ -147,7 +148,8 @@ constexpr int kBytesB = kBN * 256 * (kX == RMSMP_F32 ? 3 : 1);      // operand B
 template <bool kBulk> constexpr int kThreads = kWorkers + (kBulk ? 64 : 32);
 
 // kBulk: x comes by tensor copies (16-bit rows that start on 16 bytes and follow each other), else in the workers' hands.  (Gathered rows by tensor copies of
-// four rows: sixteen experts of 4096 x 1024 over 8192 rows 398 us, 174 by the workers.)
+// four rows: sixteen experts of 4096 x 1024 over 8192 rows 398 us, 174 by the workers.)  Eighteen warps leave 96 registers a thread; at that ptxas spills three to six words (and
+// reads two to eleven back) in the forms of 192 tokens with tensor copies and those of 256.
 template <int kBN, int kX, bool kBulk>
 __global__ void __launch_bounds__(kThreads<kBulk>, 1) gs4_tensor_kernel(const __grid_constant__ Plan p)
 {
