@@ -567,7 +567,7 @@ rmsmp_status rmsmp_expert_combine(const void* d_ys, rmsmp_dtype type, int64_t R,
 /*
  * The gradient of rmsmp_expert_combine: dys[d_place[t][j]] = w[t][j] * dy[t] and dw[t][j] = <dy[t], ys[d_place[t][j]]> (fp32 sums, a fixed order).
  * A pair without a place has dw = 0; rows of dys that no pair has are left as they were.  d_w NULL: ones.  d_dys or d_dw may be NULL if not
- * wanted (not both; d_ys may be NULL without d_dw).  Places of two pairs differ, as rmsmp_expert_sort's do: where they do not, each value of that row of
+ * wanted (not both, unless R = 0; d_ys may be NULL without d_dw).  Places of two pairs differ, as rmsmp_expert_sort's do: where they do not, each value of that row of
  * dys is that of one of the pairs, not the same one's for the whole row or from call to call (dw is not concerned).
  * Errors: as rmsmp_expert_gather.
  */

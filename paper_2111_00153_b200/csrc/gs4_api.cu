@@ -199,13 +199,13 @@ rmsmp_status rmsmp_expert_combine_backward(const void* d_dy, rmsmp_dtype type, i
                                            int64_t ld_ys, const int32_t* d_place, const float* d_w, void* d_dys, int64_t ld_dys, float* d_dw, void* stream)
 {
     NvtxRange nvtx_range("rmsmp_expert_combine_backward");
-    if (T && (!d_dy || !d_place || (!d_dys && !d_dw) || (d_dw && R && !d_ys))) return RMSMP_ERR_NULL;
+    if (T && (!d_dy || !d_place || (R && !d_dys && !d_dw) || (d_dw && R && !d_ys))) return RMSMP_ERR_NULL;      // (no rows: a gradient of none may have no address)
     const rmsmp_status ok = rows_ok(type, H, {{d_dy, T, ld_dy}, {d_ys, R, d_ys ? ld_ys : H}, {d_dys, R, d_dys ? ld_dys : H}});
     if (ok != RMSMP_OK) return ok;
     if (k < 1 || k > 1024) return RMSMP_ERR_SHAPE;
     if (!aligned(d_place, 4) || !aligned(d_w, 4) || !aligned(d_dw, 4)) return RMSMP_ERR_ALIGN;
     const rmsmp_status arch = arch_status();
-    if (arch != RMSMP_OK || T == 0) return arch;
+    if (arch != RMSMP_OK || T == 0 || (!d_dys && !d_dw)) return arch;
     return done(launch_expert_combine_backward(d_dy, type, T, k, H, ld_dy, d_ys, R, ld_ys, d_place, d_w, d_dys, ld_dys, d_dw,
                                                static_cast<cudaStream_t>(stream)));
 }

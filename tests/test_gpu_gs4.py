@@ -591,6 +591,22 @@ def test_pairs_that_share_a_place(H):
     assert np.isnan(np.delete(out, (5, 7), 0)).all()
 
 
+@pytest.mark.parametrize("H", [8, 33, 4096])
+def test_sums_back_without_any_rows(H):
+    """A capacity of none: sums and weights' gradients are zeros, and the rows' gradient, whose empty tensor has no address, is nothing."""
+    import torch
+    T, k = 7, 3
+    rows, place = torch.empty((0, H), device="cuda"), torch.arange(T * k, dtype=torch.int32, device="cuda").view(T, k)
+    w, dy = torch.ones((T, k), device="cuda"), torch.ones((T, H), device="cuda")
+    y = torch.full((T, H), float("nan"), device="cuda")
+    R.rmsmp_expert_combine(rows, R.F32, 0, H, H, place, w, T, k, y, H)
+    assert (y == 0).all()
+    for want_dw in (True, False):
+        dw = torch.full((T, k), float("nan"), device="cuda")
+        R.rmsmp_expert_combine_backward(dy, R.F32, T, k, H, H, rows, 0, H, place, w, torch.empty_like(rows), H, dw if want_dw else None)
+        assert (dw == 0).all() if want_dw else torch.isnan(dw).all()
+
+
 def test_gradients_against_differences():
     """The sum is linear in the rows and in the weights: differences of the call itself give its gradient up to rounding."""
     import torch
